@@ -43,12 +43,12 @@ def _round(n, d, dtype, fmt):
     return {"op": "round", "n": n, "d": d, "dtype": dtype, "fmt": fmt}
 
 
-def _product(m, n, d, a, b, dtype="fp32", bias=False):
-    return {"op": "product", "m": m, "n": n, "d": d, "a": a, "b": b, "dtype": dtype, "bias": bias}
+def _product(m, n, d, a, dtype="fp32", bias=False):
+    return {"op": "product", "m": m, "n": n, "d": d, "a": a, "dtype": dtype, "bias": bias}
 
 
-def _sets(n, d, l, k, fmt, empty=0.0, clusters=50):
-    return {"op": "sets", "n": n, "d": d, "l": l, "k": k, "fmt": fmt, "empty": empty, "clusters": clusters}
+def _sets(n, d, l, k, empty=0.0, clusters=50):
+    return {"op": "sets", "n": n, "d": d, "l": l, "k": k, "empty": empty, "clusters": clusters}
 
 
 def listed():
@@ -66,18 +66,19 @@ def listed():
         "round_d100_fp16": _round(50_000, 100, "fp16", "mxfp4"),
         # Rounding of the largest ground set.
         "round_large1m_fp16": _round(1_000_000, 256, "fp16", "mxfp4"),
-        # One query against a stored collection: every stored byte is read once.
-        "product_one_query": _product(1, 20_000, 1536, "mxfp8", "mxfp4"),
-        # Nothing is a multiple of anything; both sides in 8 bits, with a bias.
-        "product_ragged_fp8": _product(333, 30_011, 301, "mxfp8", "mxfp8", bias=True),
-        # A projection of many rows by 4-bit weights.
-        "product_large_fp4": _product(16_384, 8192, 4096, "mxfp4", "mxfp4", dtype="bf16"),
+        # One 8-bit query against a stored 4-bit collection: every stored byte
+        # is read once.
+        "product_one_query": _product(1, 20_000, 1536, "mxfp8"),
+        # Nothing is a multiple of anything; scores in fp32, with a bias.
+        "product_ragged_fp32": _product(333, 30_011, 301, "mxfp8", bias=True),
+        # A projection of many normalised rows (8 bits) by 4-bit weights.
+        "product_large_bf16": _product(16_384, 8192, 4096, "mxfp8", "bf16"),
         # A serving loop's few sets of different sizes on a small ground set.
-        "sets_serve_fp8": _sets(10_000, 64, 48, 8, "mxfp8", empty=0.25),
-        # Text-embedding rows in 4 bits.
-        "sets_embed_fp4": _sets(20_000, 1536, 512, 16, "mxfp4"),
-        # An optimizer's batch on a large 4-bit ground set.
-        "sets_large_fp4": _sets(200_000, 256, 512, 32, "mxfp4", clusters=100),
+        "sets_serve": _sets(10_000, 64, 48, 8, empty=0.25),
+        # Text-embedding rows.
+        "sets_embed_d1536": _sets(20_000, 1536, 512, 16),
+        # An optimizer's batch on a large ground set.
+        "sets_large": _sets(200_000, 256, 512, 32, clusters=100),
     }
     return [{"name": name, **c} for name, c in cases.items()]
 
@@ -98,16 +99,14 @@ def draw(rng):
     if op == "round":
         return _round(min(_log(rng, 1, 1_000_000), 250_000_000 // d), d, dtype, rng.choice(["mxfp4", "mxfp8"]))
     if op == "product":
-        a, b = rng.choice([("mxfp4", "mxfp4"), ("mxfp8", "mxfp4"), ("mxfp8", "mxfp8"), ("mxfp4", "mxfp8")])
         d = _log(rng, 32, 4096)
         m = _log(rng, 1, 16_384)
         n = min(_log(rng, 64, 50_000), max(64, 134_000_000 // m))
-        return _product(m, n, d, a, b, dtype, rng.random() < 0.5)
+        return _product(m, n, d, rng.choice(["mxfp4", "mxfp8"]), dtype, rng.random() < 0.5)
     d, n = _log(rng, 16, 2048), _log(rng, 1000, 200_000)
     l, k = _log(rng, 16, 1024), _log(rng, 1, 48)
     l = max(1, min(l, int(min(1.6e12 / (2.0 * n * k * d), 3.2e9 / (n * k)))))
-    return _sets(n, d, l, k, rng.choice(["mxfp4", "mxfp8"]), rng.choice([0.0, 0.0, 0.3]) if k > 1 else 0.0,
-                 rng.choice([0, 10, 50]))
+    return _sets(n, d, l, k, rng.choice([0.0, 0.0, 0.3]), rng.choice([0, 10, 50]))
 
 
 # -- plain forms, in 32 bits ---------------------------------------------------
@@ -185,7 +184,7 @@ def prepare(case, seed):
     s = {"c": dict(case)}
     if c["op"] == "sets":
         n, l, k = c["n"], c["l"], c["k"]
-        s["V"] = _stored(_points(c, g), c["fmt"])
+        s["V"] = _stored(_points(c, g), "mxfp4")
         sets = torch.randint(0, n, (l, k), generator=g, device="cuda", dtype=torch.int32)
         if c["empty"]:
             blank = torch.rand(l, k, generator=g, device="cuda") < c["empty"]
@@ -194,7 +193,7 @@ def prepare(case, seed):
         return s
     if c["op"] == "product":
         s["A"] = _stored(_randn(g, c["m"], c["d"]), c["a"])
-        s["B"] = _stored(_randn(g, c["n"], c["d"]) / math.sqrt(c["d"]), c["b"])
+        s["B"] = _stored(_randn(g, c["n"], c["d"]) / math.sqrt(c["d"]), "mxfp4")
         s["bias"] = _randn(g, c["n"]) if c["bias"] else None
         return s
     n, d, T = c["n"], c["d"], DTYPES[c["dtype"]]
@@ -240,10 +239,10 @@ def _plain(s):
     if c["op"] == "round":
         return _values(*_round_rows(s["x"].float(), c["fmt"]), d).to(T)
     if c["op"] == "product":
-        C = _loaded(s["A"], d, c["a"]) @ _loaded(s["B"], d, c["b"]).t()
+        C = _loaded(s["A"], d, c["a"]) @ _loaded(s["B"], d, "mxfp4").t()
         return (C if s["bias"] is None else C + s["bias"]).to(T)
     # f(S) = (2/n) sum_v max(0, max_s <v, s> - |s|^2 / 2)
-    V, sets = _loaded(s["V"], d, c["fmt"]), s["sets"]
+    V, sets = _loaded(s["V"], d, "mxfp4"), s["sets"]
     E = V[sets.clamp(min=0).flatten().long()]
     bias = torch.where(sets.flatten() >= 0, -0.5 * E.square().sum(1), -math.inf)
     H = (V @ E.t()).add_(bias).view(c["n"], c["l"], c["k"])
@@ -255,7 +254,8 @@ def _own(s):
 
     c, d = s["c"], s["c"]["d"]
     T = DTYPES.get(c.get("dtype", "fp32"))
-    fmt = {"mxfp4": api.EXEMCL_MXFP4, "mxfp8": api.EXEMCL_MXFP8, "none": None}
+    fp4 = api.EXEMCL_MXFP4
+    fmt = {"mxfp4": fp4, "mxfp8": api.EXEMCL_MXFP8, "none": None}
     if c["op"] == "norm":
         y, h, rstd = api.exemplar_rmsnorm(s["x"], s["w"], s["r"], eps=EPS, format=fmt[c["fmt"]])
         more = [] if s["r"] is None else [h]
@@ -270,9 +270,9 @@ def _own(s):
     if c["op"] == "round":
         return api.exemplar_mx_dequantize(api.exemplar_mx_quantize(s["x"], fmt[c["fmt"]]), T)
     if c["op"] == "product":
-        return api.exemplar_mx_product(api.MxRows(*s["A"], d, fmt[c["a"]]), api.MxRows(*s["B"], d, fmt[c["b"]]),
+        return api.exemplar_mx_product(api.MxRows(*s["A"], d, fmt[c["a"]]), api.MxRows(*s["B"], d, fp4),
                                        bias=s["bias"], dtype=T)
-    return api.exemplar_mx_eval(api.MxRows(*s["V"], d, fmt[c["fmt"]]), s["sets"])
+    return api.exemplar_mx_eval(api.MxRows(*s["V"], d, fp4), s["sets"])
 
 
 def run(state):
@@ -298,10 +298,10 @@ def work(case):
         return {"bytes": 2.0 * c["n"] * d * es, "flops": 4.0 * c["n"] * d}
     if c["op"] == "product":
         m, n = c["m"], c["n"]
-        return {"bytes": _mx_bytes(m, d, c["a"]) + _mx_bytes(n, d, c["b"]) + (4 * n if c["bias"] else 0) + m * n * es,
+        return {"bytes": _mx_bytes(m, d, c["a"]) + _mx_bytes(n, d, "mxfp4") + (4 * n if c["bias"] else 0) + m * n * es,
                 "flops": 2.0 * m * n * d}
     n, l, k = c["n"], c["l"], c["k"]
-    return {"bytes": _mx_bytes(n, d, c["fmt"]) + 4 * l * k + 4 * l, "flops": 2.0 * n * l * k * d}
+    return {"bytes": _mx_bytes(n, d, "mxfp4") + 4 * l * k + 4 * l, "flops": 2.0 * n * l * k * d}
 
 
 # -- the definition in 64 bits -------------------------------------------------------
@@ -376,9 +376,9 @@ def exact(case, seed):
             dx = dx + s["dh"].double()
         return [dx, ((dy * h) * rstd[:, None]).sum(0)]
     if c["op"] == "product":
-        C = _exact_values(s["A"], d, c["a"]) @ _exact_values(s["B"], d, c["b"]).t().contiguous()
+        C = _exact_values(s["A"], d, c["a"]) @ _exact_values(s["B"], d, "mxfp4").t().contiguous()
         return C if s["bias"] is None else C + s["bias"].double()
-    V, sets, n, k = _exact_values(s["V"], d, c["fmt"]), s["sets"], c["n"], c["k"]
+    V, sets, n, k = _exact_values(s["V"], d, "mxfp4"), s["sets"], c["n"], c["k"]
     half = 0.5 * (V * V).sum(1)
     f = torch.zeros(c["l"], dtype=torch.float64, device="cuda")
     rows = max(1, 400_000_000 // (c["l"] * k))
