@@ -280,6 +280,135 @@ EXEMCL_API int exemplar_greedy(const float *V, int64_t n, int64_t d, int64_t K, 
 EXEMCL_API int exemplar_sqnorm(const void *V, int64_t n, int64_t d, int precision, float *q,
                                void *stream);
 
+/* ------------------------------------------------------------------------
+ * Microscaled rows: rows of 8- or 4-bit floating-point elements with one
+ * power-of-two scale per 32 consecutive coordinates (the OCP microscaling
+ * formats MXFP8 with E4M3 elements and MXFP4 with E2M1 elements), and what
+ * makes and uses them: embeddings as they leave a model's last norm, stored in
+ * a half to an eighth of their bytes.
+ *
+ * A matrix of n rows of d coordinates (1 <= d <= 2^22) is two dense arrays,
+ * both padded per row to dp = d rounded up to a multiple of 128:
+ *   codes   n x dp bytes (8 bits: bit 7 sign, 4 exponent, 3 mantissa bits,
+ *           bias 7, largest 448, 0x7f and 0xff NaN) or n x dp/2 bytes (4 bits:
+ *           sign, 2 exponent, 1 mantissa bits, +-{0, .5, 1, 1.5, 2, 3, 4, 6};
+ *           the even coordinate in the low nibble).  16-byte aligned.  Codes
+ *           past d are zeros.
+ *   scales  n x dp/32 bytes: s stands for 2^(s - 127), 255 for NaN, for the
+ *           whole block.  4-byte aligned.  Not 255 past d.
+ * exemplar_mx_layout gives the row sizes.  The conventions above (ownership,
+ * streams, asynchrony) hold for these calls too, but n may be 0 (nothing is
+ * queued then, and the arrays may be NULL), and infinities and NaN are defined
+ * where a call says so.  Outputs must not overlap inputs unless a call says
+ * that they may.
+ * ------------------------------------------------------------------------ */
+enum exemcl_mx_format {
+    EXEMCL_MX_NONE = 0, /* exemplar_rmsnorm only: rows of the input's type */
+    EXEMCL_MXFP4 = 4,
+    EXEMCL_MXFP8 = 8
+};
+
+/*
+ * exemplar_mx_layout -- bytes of one row of codes and of one row of scales
+ * (either pointer may be NULL); host only.  EINVAL for d < 1, d > 2^22 or an
+ * unknown format.
+ */
+EXEMCL_API int exemplar_mx_layout(int64_t d, int format, int64_t *row_bytes, int64_t *row_scales);
+
+/*
+ * exemplar_mx_quantize -- rounds n rows of d coordinates.
+ *
+ * A block whose largest magnitude is a gets the scale 2^X, X = floor(log2 a) -
+ * 2 (4 bits) or - 8 (8 bits), not below 2^-127; its elements are v / 2^X
+ * rounded to nearest, ties to even, and at most the format's largest value (the
+ * conversion of the OCP specification).  A block that holds an infinity or a
+ * NaN gets the scale 255: all of it reads as NaN.
+ *
+ *   x               device, n x d row-major, type per `precision`
+ *   codes, scales   device; written, padding included
+ */
+EXEMCL_API int exemplar_mx_quantize(const void *x, int64_t n, int64_t d, int precision, int format, void *codes,
+                                    void *scales, void *stream);
+
+/*
+ * exemplar_mx_dequantize -- the values of n rows, as n x d elements of type
+ * `precision` (exact in fp32 and bf16 down to their subnormal numbers; fp16
+ * rounds, and what is past its range becomes infinite).
+ */
+EXEMCL_API int exemplar_mx_dequantize(const void *codes, const void *scales, int64_t n, int64_t d, int format,
+                                      int precision, void *x, void *stream);
+
+/*
+ * exemplar_rmsnorm -- root-mean-square norm of n rows, with the residual's
+ * addition before it and the rounding to microscaled rows behind it:
+ *   v = x + residual,  y = v * weight / sqrt(mean(v^2) + eps).
+ * Everything is computed in fp32 from the unrounded sum v.
+ *
+ *   x, residual  device, n x d row-major, type per `precision`; residual may be
+ *                NULL (v = x)
+ *   weight       device, d elements of the same type; NULL: all 1
+ *   eps          >= 0, finite
+ *   format       EXEMCL_MX_NONE: y is n x d elements of the same type and
+ *                `scales` is ignored; else y and scales are codes and scales
+ *                (d <= 2^22)
+ *   h            device, n x d of the same type, v rounded; may be NULL, and may
+ *                be x or residual itself
+ *   rstd         device, n floats, 1 / sqrt(mean(v^2) + eps); may be NULL
+ */
+EXEMCL_API int exemplar_rmsnorm(const void *x, const void *residual, const void *weight, int64_t n, int64_t d,
+                                int precision, float eps, int format, void *h, void *y, void *scales, float *rstd,
+                                void *stream);
+
+/*
+ * exemplar_rmsnorm_backward -- gradient of y = v * weight * rstd (the rounding
+ * to microscaled rows counts as the identity): with xhat = h * rstd and
+ * g = dy * weight,
+ *   dx = rstd * (g - xhat * mean(g * xhat)) + dh,   dweight = sum_rows dy * xhat.
+ * dx is the gradient of x and of the residual alike.
+ *
+ *   dy, h    device, n x d, type per `precision`; h as exemplar_rmsnorm wrote it
+ *   weight   device, d elements; NULL: all 1
+ *   rstd     device, n floats, as exemplar_rmsnorm wrote them
+ *   dh       device, n x d: the gradient that reaches v past the norm; may be
+ *            NULL
+ *   dx       device, n x d; written
+ *   dweight  device, d floats; written (zeros where n = 0); may be NULL
+ *
+ * Sums over the rows are taken in a fixed order, so the result is bitwise
+ * reproducible.  Temporary memory: up to 1 024 x d floats.
+ */
+EXEMCL_API int exemplar_rmsnorm_backward(const void *dy, const void *h, const void *weight, const float *rstd,
+                                         const void *dh, int64_t n, int64_t d, int precision, void *dx, float *dweight,
+                                         void *stream);
+
+/*
+ * exemplar_mx_product -- C[i][j] = sum_t A[i][t] * B[j][t] + bias[j].
+ *
+ *   A, A_scales  device, m rows of `format_a`
+ *   B, B_scales  device, n rows of 4 bits (EXEMCL_MXFP4)
+ *   d            coordinates of the rows of both
+ *   bias         device, n floats; may be NULL
+ *   precision    of C: fp32, or rounded to fp16 / bf16
+ *   C            device, m x n row-major; written
+ *
+ * Sums of 4-bit products are exact up to fp32's rounding.  With 8-bit rows and
+ * fp32 results they are taken in two parts, to the same end; with 16-bit
+ * results in one, whose error is about 1e-5 of the result's size, below 1/100
+ * of a 16-bit rounding.  A NaN block makes its row's or column's results NaN.
+ */
+EXEMCL_API int exemplar_mx_product(const void *A, const void *A_scales, int64_t m, int format_a, const void *B,
+                                   const void *B_scales, int64_t n, int64_t d, const float *bias, int precision, void *C,
+                                   void *stream);
+
+/*
+ * exemplar_mx_eval -- exemplar_eval for a V of 4-bit rows (EXEMCL_MXFP4): out[j]
+ * = f(S_j) of the values that V's rows stand for.  Empty slots, invalid indices,
+ * k = 0, l = 0 and reproducibility as there; a NaN block in V gives unspecified
+ * results.
+ */
+EXEMCL_API int exemplar_mx_eval(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets,
+                                int64_t l, int64_t k, float *out, void *stream);
+
 /*
  * exemplar_plan -- host-only description of what exemplar_eval would launch
  * for these sizes; touches no device.  Writes the chosen exemcl_path to

@@ -9,18 +9,21 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import Any, NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libexemcl.so")
 
 EXEMCL_FP32, EXEMCL_FP16, EXEMCL_BF16 = 0, 1, 2
+EXEMCL_MX_NONE, EXEMCL_MXFP4, EXEMCL_MXFP8 = 0, 4, 8
 EXEMCL_OK, EXEMCL_EINVAL, EXEMCL_ENOMEM, EXEMCL_EDEVICE, EXEMCL_ESCRATCH = 0, 1, 2, 3, 4
 EXEMCL_SCRATCH_BYTES = 64 << 20   # fixed scratch buffer of exemplar_eval_noalloc
 PATH_NONE, PATH_VALU, PATH_MFMA = 0, 1, 2
 PATH_NAMES = {PATH_NONE: "none", PATH_VALU: "valu", PATH_MFMA: "mfma"}
 
 EXPORTED = ("exemplar_eval", "exemplar_eval_noalloc", "exemplar_eval_streamed", "exemplar_gain", "exemplar_greedy", "exemplar_sqnorm",
-            "exemplar_plan",
+            "exemplar_plan", "exemplar_mx_layout", "exemplar_mx_quantize", "exemplar_mx_dequantize", "exemplar_rmsnorm",
+            "exemplar_rmsnorm_backward", "exemplar_mx_product", "exemplar_mx_eval",
             "exemplar_prof_enable", "exemplar_prof_read", "exemplar_strerror", "exemplar_version")
 
 
@@ -60,6 +63,21 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.exemplar_plan.argtypes = [i64, i64, i64, i64, ip, ctypes.POINTER(ctypes.c_int),
                                   ctypes.POINTER(ctypes.c_int64)]
     lib.exemplar_plan.restype = ip
+    fl = ctypes.c_float
+    lib.exemplar_mx_layout.argtypes = [i64, ip, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)]
+    lib.exemplar_mx_layout.restype = ip
+    lib.exemplar_mx_quantize.argtypes = [vp, i64, i64, ip, ip, vp, vp, vp]
+    lib.exemplar_mx_quantize.restype = ip
+    lib.exemplar_mx_dequantize.argtypes = [vp, vp, i64, i64, ip, ip, vp, vp]
+    lib.exemplar_mx_dequantize.restype = ip
+    lib.exemplar_rmsnorm.argtypes = [vp, vp, vp, i64, i64, ip, fl, ip, vp, vp, vp, vp, vp]
+    lib.exemplar_rmsnorm.restype = ip
+    lib.exemplar_rmsnorm_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, ip, vp, vp, vp]
+    lib.exemplar_rmsnorm_backward.restype = ip
+    lib.exemplar_mx_product.argtypes = [vp, vp, i64, ip, vp, vp, i64, i64, vp, ip, vp, vp]
+    lib.exemplar_mx_product.restype = ip
+    lib.exemplar_mx_eval.argtypes = [vp, vp, i64, i64, vp, i64, i64, vp, vp]
+    lib.exemplar_mx_eval.restype = ip
     lib.exemplar_strerror.argtypes = [ip]
     lib.exemplar_strerror.restype = ctypes.c_char_p
     lib.exemplar_prof_enable.argtypes = [ip]
@@ -266,6 +284,198 @@ def exemplar_sqnorm(V, out=None, stream=None):
         rc = load().exemplar_sqnorm(_ptr(V), n, d, prec, _ptr(out), _stream(stream))
     if rc != EXEMCL_OK:
         raise ExemclError(rc, "exemplar_sqnorm")
+    return out
+
+
+class MxRows(NamedTuple):
+    """Rows of ``d`` coordinates as 8- or 4-bit elements with a power-of-two
+    scale per 32 of them (the layout is in exemcl.h): uint8 tensors ``codes``
+    (n x row bytes) and ``scales`` (n x dp/32), and the format, EXEMCL_MXFP4 or
+    EXEMCL_MXFP8."""
+    codes: Any
+    scales: Any
+    d: int
+    format: int
+
+
+def _mx_row(d: int, format: int):
+    """(code bytes, scale bytes) of one stored row."""
+    if format not in (EXEMCL_MXFP4, EXEMCL_MXFP8):
+        raise ValueError("format must be EXEMCL_MXFP4 or EXEMCL_MXFP8")
+    if not 1 <= d <= 1 << 22:
+        raise ValueError("microscaled rows have 1 to 2^22 coordinates")
+    dp = (d + 127) // 128 * 128
+    return dp * format // 8, dp // 32
+
+
+def _mx_check(q, name):
+    """The rows of q, after its tensors' types and shapes were checked."""
+    import torch
+    rb, rs = _mx_row(q.d, q.format)
+    for t, width in ((q.codes, rb), (q.scales, rs)):
+        if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[1] != width:
+            raise ValueError(f"{name}: codes must be uint8 n x {rb} and scales uint8 n x {rs}")
+    if q.codes.shape[0] != q.scales.shape[0]:
+        raise ValueError(f"{name}: codes and scales have different numbers of rows")
+    return q.codes.shape[0]
+
+
+def _mx_empty(n, d, format, device):
+    import torch
+    rb, rs = _mx_row(d, format)
+    return MxRows(torch.empty((n, rb), dtype=torch.uint8, device=device),
+                  torch.empty((n, rs), dtype=torch.uint8, device=device), d, format)
+
+
+def exemplar_mx_layout(d: int, format: int):
+    """(code bytes, scale bytes) of one row of d coordinates; host only."""
+    rb, rs = ctypes.c_int64(-1), ctypes.c_int64(-1)
+    rc = load().exemplar_mx_layout(d, format, ctypes.byref(rb), ctypes.byref(rs))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, "exemplar_mx_layout")
+    return int(rb.value), int(rs.value)
+
+
+def exemplar_mx_quantize(x, format, out=None, stream=None):
+    """The rows of x (n x d) rounded to MxRows of ``format`` (see
+    exemplar_mx_quantize in exemcl.h)."""
+    if x.dim() != 2:
+        raise ValueError("x must be n x d")
+    prec = precision_of(x.dtype)
+    n, d = x.shape
+    if out is None:
+        out = _mx_empty(n, d, format, x.device)
+    elif out.d != d or out.format != format or _mx_check(out, "out") != n:
+        raise ValueError("out must be MxRows of x's shape and the format")
+    with _device_scope(_check_device(x, out.codes, out.scales)):
+        rc = load().exemplar_mx_quantize(_ptr(x), n, d, prec, format, _ptr(out.codes), _ptr(out.scales), _stream(stream))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, "exemplar_mx_quantize")
+    return out
+
+
+def exemplar_mx_dequantize(q, dtype, out=None, stream=None):
+    """The values of MxRows q as an n x d tensor of ``dtype`` (see
+    exemplar_mx_dequantize in exemcl.h)."""
+    import torch
+    prec = precision_of(dtype)
+    n = _mx_check(q, "q")
+    if out is None:
+        out = torch.empty((n, q.d), dtype=dtype, device=q.codes.device)
+    elif out.dtype != dtype or out.shape != (n, q.d):
+        raise ValueError("out must be an n x d tensor of the dtype")
+    with _device_scope(_check_device(q.codes, q.scales, out)):
+        rc = load().exemplar_mx_dequantize(_ptr(q.codes), _ptr(q.scales), n, q.d, q.format, prec, _ptr(out),
+                                           _stream(stream))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, "exemplar_mx_dequantize")
+    return out
+
+
+def exemplar_rmsnorm(x, weight=None, residual=None, eps=1e-6, format=None, stream=None):
+    """(y, h, rstd): v = x + residual, h = v in x's type (x itself without a
+    residual), y = v * weight / sqrt(mean(v^2) + eps) as a tensor of x's type,
+    or as MxRows of ``format``, and rstd = 1 / sqrt(...) in float32 (see
+    exemplar_rmsnorm in exemcl.h)."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must be n x d")
+    prec = precision_of(x.dtype)
+    n, d = x.shape
+    if weight is not None and (weight.dtype != x.dtype or weight.shape != (d,)):
+        raise ValueError("weight must have x's type and d elements")
+    if residual is not None and (residual.dtype != x.dtype or residual.shape != x.shape):
+        raise ValueError("residual must have x's type and shape")
+    h = x if residual is None else torch.empty_like(x, memory_format=torch.contiguous_format)
+    rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    if format is None or format == EXEMCL_MX_NONE:
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        codes, scales, fmt = y, None, EXEMCL_MX_NONE
+    else:
+        y = _mx_empty(n, d, format, x.device)
+        codes, scales, fmt = y.codes, y.scales, format
+    with _device_scope(_check_device(x, residual, weight, codes)):
+        rc = load().exemplar_rmsnorm(_ptr(x), _ptr(residual), _ptr(weight), n, d, prec, eps, fmt,
+                                     _ptr(None if residual is None else h), _ptr(codes), _ptr(scales), _ptr(rstd),
+                                     _stream(stream))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, "exemplar_rmsnorm")
+    return y, h, rstd
+
+
+def exemplar_rmsnorm_backward(dy, h, weight, rstd, dh=None, stream=None):
+    """(dx, dweight) of exemplar_rmsnorm from the gradient dy of y, the h and
+    rstd it returned, and dh, the gradient that reaches h another way; dx is
+    the gradient of x and of the residual, dweight is float32 (see
+    exemplar_rmsnorm_backward in exemcl.h)."""
+    import torch
+    if h.dim() != 2:
+        raise ValueError("h must be n x d")
+    prec = precision_of(h.dtype)
+    n, d = h.shape
+    for t, name in ((dy, "dy"), (dh, "dh")):
+        if t is not None and (t.dtype != h.dtype or t.shape != h.shape):
+            raise ValueError(f"{name} must have h's type and shape")
+    if weight is not None and (weight.dtype != h.dtype or weight.shape != (d,)):
+        raise ValueError("weight must have h's type and d elements")
+    if rstd.dtype != torch.float32 or rstd.shape != (n,):
+        raise ValueError("rstd must be float32 with n elements")
+    dx = torch.empty_like(h, memory_format=torch.contiguous_format)
+    dw = torch.empty(d, dtype=torch.float32, device=h.device)
+    with _device_scope(_check_device(h, dy, weight, rstd, dh)):
+        rc = load().exemplar_rmsnorm_backward(_ptr(dy), _ptr(h), _ptr(weight), _ptr(rstd), _ptr(dh), n, d, prec, _ptr(dx),
+                                              _ptr(dw), _stream(stream))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, "exemplar_rmsnorm_backward")
+    return dx, dw
+
+
+def exemplar_mx_product(A, B, bias=None, dtype=None, out=None, stream=None):
+    """C[i][j] = <A_i, B_j> + bias[j] for MxRows A (m rows of 8 or 4 bits) and
+    B (n rows of 4 bits), as an m x n tensor of ``dtype`` (default float32; see
+    exemplar_mx_product in exemcl.h)."""
+    import torch
+    dtype = torch.float32 if dtype is None else dtype
+    prec = precision_of(dtype)
+    m, n = _mx_check(A, "A"), _mx_check(B, "B")
+    if A.d != B.d:
+        raise ValueError("A and B must have the same number of coordinates")
+    if B.format != EXEMCL_MXFP4:
+        raise ValueError("B must be EXEMCL_MXFP4 rows")
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,)):
+        raise ValueError("bias must be float32 with one element per row of B")
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype, device=A.codes.device)
+    elif out.dtype != dtype or out.shape != (m, n):
+        raise ValueError("out must be an m x n tensor of the dtype")
+    with _device_scope(_check_device(A.codes, A.scales, B.codes, B.scales, bias, out)):
+        rc = load().exemplar_mx_product(_ptr(A.codes), _ptr(A.scales), m, A.format, _ptr(B.codes), _ptr(B.scales), n, A.d,
+                                        _ptr(bias), prec, _ptr(out), _stream(stream))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, "exemplar_mx_product")
+    return out
+
+
+def exemplar_mx_eval(V, sets, out=None, stream=None):
+    """out[j] = f(S_j) for MxRows V of 4 bits and the l x k int32 index matrix
+    ``sets`` (see exemplar_mx_eval in exemcl.h)."""
+    import torch
+    n = _mx_check(V, "V")
+    if V.format != EXEMCL_MXFP4:
+        raise ValueError("V must be EXEMCL_MXFP4 rows")
+    if sets.dim() != 2:
+        raise ValueError("sets must be l x k")
+    if sets.dtype != torch.int32:
+        raise TypeError("sets must be int32")
+    l, k = sets.shape
+    if out is None:
+        out = torch.empty(l, dtype=torch.float32, device=V.codes.device)
+    elif out.dtype != torch.float32 or out.numel() != l:
+        raise ValueError("out must be float32 with l elements")
+    with _device_scope(_check_device(V.codes, V.scales, sets, out)):
+        rc = load().exemplar_mx_eval(_ptr(V.codes), _ptr(V.scales), n, V.d, _ptr(sets), l, k, _ptr(out), _stream(stream))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, "exemplar_mx_eval")
     return out
 
 

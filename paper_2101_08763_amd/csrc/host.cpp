@@ -1,5 +1,6 @@
 // host.cpp -- the C ABI declared in include/exemcl.h: argument validation,
 // path selection, stream-ordered temporary memory, kernel sequencing.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stdlib.h>
@@ -13,6 +14,7 @@
 
 #include "exemcl.h"
 #include "internal.h"
+#include "mx_layout.hpp"
 
 using namespace exemcl;
 
@@ -847,6 +849,44 @@ int scratch_arena(Arena *a) {
     return EXEMCL_OK;
 }
 
+// f of l sets of k 4-bit rows, in chunks of whole set groups where the
+// temporary memory for all of them is not to be had (as in run_eval).
+int run_mx_eval(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets, int64_t l, int64_t k,
+                float *out, hipStream_t st) {
+    if (l == 0) return EXEMCL_OK;
+    if (k == 0) return status_of(launch_zero(out, l, st));
+    const int64_t G = mx_sets_parts(n, d), unit = kMxSets, limit = workspace_limit();
+    int64_t lc = l, lpad = 0, off = 0;
+    Scratch ws;
+    for (;;) {
+        lpad = align_up(lc, unit);
+        off = align_up(lc * k * 4, 256);
+        const int64_t bytes = off + G * lpad * 4;
+        const int rc = bytes <= limit ? alloc_scratch(&ws, bytes, st) : EXEMCL_ENOMEM;
+        if (rc == EXEMCL_OK) break;
+        if (rc != EXEMCL_ENOMEM || lc <= unit) return rc;
+        lc = align_up((lc + 1) / 2, unit);
+    }
+    float *biases = (float *)ws.ptr, *partials = (float *)((char *)ws.ptr + off);
+    for (int64_t j0 = 0; j0 < l; j0 += lc) {
+        const int64_t lj = std::min(lc, l - j0);
+        hipError_t e = launch_mx_sets(codes, scales, n, d, sets + j0 * k, lj, k, biases, partials, lpad, st);
+        if (e == hipSuccess) e = launch_reduce(partials, G, lpad, lj, n, sets + j0 * k, k, nullptr, 0, out + j0, st);
+        if (e != hipSuccess) return EXEMCL_EDEVICE;
+    }
+    return EXEMCL_OK;
+}
+
+// Arguments every call on microscaled rows checks.
+bool mx_format_ok(int f) { return f == EXEMCL_MXFP4 || f == EXEMCL_MXFP8; }
+
+bool rows_ok(int64_t n, int64_t d, int64_t max_d) { return n >= 0 && n <= INT32_MAX && d >= 1 && d <= max_d; }
+
+// The arrays of n microscaled rows: there, and aligned.
+bool mx_rows_ok(const void *codes, const void *scales, int64_t n) {
+    return n == 0 || (codes && scales && (uintptr_t)codes % 16 == 0 && (uintptr_t)scales % 4 == 0);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1137,6 +1177,81 @@ EXEMCL_API int exemplar_sqnorm(const void *V, int64_t n, int64_t d, int precisio
     if (n < 1 || n > INT32_MAX || d < 1 || d > INT32_MAX) return EXEMCL_EINVAL;
     if (!prec_ok(precision)) return EXEMCL_EINVAL;
     return status_of(launch_sqnorm(precision, V, n, (int)d, q, (hipStream_t)stream));
+}
+
+EXEMCL_API int exemplar_mx_layout(int64_t d, int format, int64_t *row_bytes, int64_t *row_scales) {
+    if (d < 1 || d > kMxMaxD || !mx_format_ok(format)) return EXEMCL_EINVAL;
+    if (row_bytes) *row_bytes = mx_row_bytes(d, format);
+    if (row_scales) *row_scales = mx_row_scales(d);
+    return EXEMCL_OK;
+}
+
+EXEMCL_API int exemplar_mx_quantize(const void *x, int64_t n, int64_t d, int precision, int format, void *codes,
+                                    void *scales, void *stream) {
+    if (!rows_ok(n, d, kMxMaxD) || !prec_ok(precision) || !mx_format_ok(format)) return EXEMCL_EINVAL;
+    if ((n > 0 && !x) || !mx_rows_ok(codes, scales, n)) return EXEMCL_EINVAL;
+    return status_of(launch_mx_quantize(precision, format, x, n, d, codes, scales, (hipStream_t)stream));
+}
+
+EXEMCL_API int exemplar_mx_dequantize(const void *codes, const void *scales, int64_t n, int64_t d, int format,
+                                      int precision, void *x, void *stream) {
+    if (!rows_ok(n, d, kMxMaxD) || !prec_ok(precision) || !mx_format_ok(format)) return EXEMCL_EINVAL;
+    if ((n > 0 && !x) || !mx_rows_ok(codes, scales, n)) return EXEMCL_EINVAL;
+    return status_of(launch_mx_dequantize(precision, format, codes, scales, n, d, x, (hipStream_t)stream));
+}
+
+EXEMCL_API int exemplar_rmsnorm(const void *x, const void *residual, const void *weight, int64_t n, int64_t d,
+                                int precision, float eps, int format, void *h, void *y, void *scales, float *rstd,
+                                void *stream) {
+    const bool mx = mx_format_ok(format);
+    if (!mx && format != EXEMCL_MX_NONE) return EXEMCL_EINVAL;
+    if (!rows_ok(n, d, mx ? kMxMaxD : kMaxNormD) || !prec_ok(precision)) return EXEMCL_EINVAL;
+    if (!(eps >= 0.0f) || eps > FLT_MAX) return EXEMCL_EINVAL;
+    if (n > 0 && (!x || !y)) return EXEMCL_EINVAL;
+    if (mx && !mx_rows_ok(y, scales, n)) return EXEMCL_EINVAL;
+    const NormArgs a{x, residual, weight, n, d, eps, h, y, scales, rstd};
+    return status_of(launch_rmsnorm(precision, format, a, (hipStream_t)stream));
+}
+
+EXEMCL_API int exemplar_rmsnorm_backward(const void *dy, const void *h, const void *weight, const float *rstd,
+                                         const void *dh, int64_t n, int64_t d, int precision, void *dx, float *dweight,
+                                         void *stream) {
+    if (!rows_ok(n, d, kMaxNormD) || !prec_ok(precision)) return EXEMCL_EINVAL;
+    if (n > 0 && (!dy || !h || !rstd || !dx)) return EXEMCL_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    if (n == 0) return dweight ? status_of(launch_zero(dweight, d, st)) : EXEMCL_OK;
+    NormGradArgs a{dy, h, weight, rstd, dh, n, d, rmsnorm_grad_parts(n, d), dx, dweight, nullptr};
+    Scratch ws;
+    if (dweight) {
+        const int64_t bytes = a.parts * d * 4;
+        if (bytes > workspace_limit()) return EXEMCL_ENOMEM;
+        const int rc = alloc_scratch(&ws, bytes, st);
+        if (rc) return rc;
+        a.partial = (float *)ws.ptr;
+    }
+    return status_of(launch_rmsnorm_grad(precision, a, st));
+}
+
+EXEMCL_API int exemplar_mx_product(const void *A, const void *A_scales, int64_t m, int format_a, const void *B,
+                                   const void *B_scales, int64_t n, int64_t d, const float *bias, int precision, void *C,
+                                   void *stream) {
+    if (!rows_ok(m, d, kMxMaxD) || !rows_ok(n, d, kMxMaxD)) return EXEMCL_EINVAL;
+    if (!prec_ok(precision) || !mx_format_ok(format_a)) return EXEMCL_EINVAL;
+    if (!mx_rows_ok(A, A_scales, m) || !mx_rows_ok(B, B_scales, n)) return EXEMCL_EINVAL;
+    if (m == 0 || n == 0) return EXEMCL_OK;
+    if (!C) return EXEMCL_EINVAL;
+    const MxProductArgs a{A, A_scales, m, format_a, B, B_scales, n, d, bias, C};
+    return status_of(format_a == EXEMCL_MXFP4 ? mx_product_fp4(precision, a, (hipStream_t)stream)
+                                              : mx_product_fp8(precision, a, (hipStream_t)stream));
+}
+
+EXEMCL_API int exemplar_mx_eval(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets,
+                                int64_t l, int64_t k, float *out, void *stream) {
+    const int rc = check_common(codes, n, d, l, k, out);
+    if (rc) return rc;
+    if (d > kMxMaxD || !mx_rows_ok(codes, scales, n)) return EXEMCL_EINVAL;
+    if (l > 0 && k > 0 && !sets) return EXEMCL_EINVAL;
+    return run_mx_eval(codes, scales, n, d, sets, l, k, out, (hipStream_t)stream);
 }
 
 EXEMCL_API int exemplar_plan(int64_t n, int64_t d, int64_t l, int64_t k, int precision, int *path,

@@ -222,4 +222,56 @@ hipError_t launch_greedy_pick(const int32_t *probes, const float *probe_scores, 
 hipError_t launch_argmax(const float *scores, uint8_t *taken, int64_t n, float *pval, int32_t *pidx,
                          int32_t *S_slot, float *f_slot, hipStream_t st);
 
+// ---------------------------------------------------------------------------
+// Microscaled rows (mx_device.hpp has the layout; `bits`: 4 or 8).
+// ---------------------------------------------------------------------------
+hipError_t launch_mx_quantize(int prec, int bits, const void *x, int64_t n, int64_t d, void *codes, void *scales,
+                              hipStream_t st);
+hipError_t launch_mx_dequantize(int prec, int bits, const void *codes, const void *scales, int64_t n, int64_t d, void *x,
+                                hipStream_t st);
+
+// v = x + residual, y = v * weight / sqrt(mean(v^2) + eps); null: no residual,
+// weights of 1, no v (h) or 1 / sqrt (rstd) wanted.  y: rows of x's type
+// (format 0) or codes, with `scales`.
+struct NormArgs {
+    const void *x, *residual, *weight;
+    int64_t n, d;
+    float eps;
+    void *h, *y, *scales;
+    float *rstd;
+};
+hipError_t launch_rmsnorm(int prec, int format, const NormArgs &a, hipStream_t st);
+
+// Its gradient; partial: parts x d floats, parts = rmsnorm_grad_parts(n, d).
+struct NormGradArgs {
+    const void *dy, *h, *weight;
+    const float *rstd;
+    const void *dh;
+    int64_t n, d, parts;
+    void *dx;
+    float *dw, *partial;
+};
+int64_t rmsnorm_grad_parts(int64_t n, int64_t d);
+hipError_t launch_rmsnorm_grad(int prec, const NormGradArgs &a, hipStream_t st);
+
+// C[i][j] = <A_i, B_j> + bias[j] (bias nullable); B of 4 bits.
+struct MxProductArgs {
+    const void *A, *A_scales;
+    int64_t m;
+    int bits_a;
+    const void *B, *B_scales;
+    int64_t n, d;
+    const float *bias;
+    void *C;
+};
+hipError_t mx_product_fp4(int prec, const MxProductArgs &a, hipStream_t st);
+hipError_t mx_product_fp8(int prec, const MxProductArgs &a, hipStream_t st);
+
+// Sets on 4-bit rows: biases[l * k] = -||s||^2 / 2 of every slot's row
+// (-FLT_MAX: empty or invalid), and partials as launch_mfma writes them, G =
+// mx_sets_parts(n, d) rows of lpad.
+int64_t mx_sets_parts(int64_t n, int64_t d);
+hipError_t launch_mx_sets(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets, int64_t l,
+                          int64_t k, float *biases, float *partials, int64_t lpad, hipStream_t st);
+
 }  // namespace exemcl
