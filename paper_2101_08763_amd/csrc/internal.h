@@ -267,11 +267,12 @@ struct MxProductArgs {
 hipError_t mx_product_fp4(int prec, const MxProductArgs &a, hipStream_t st);
 hipError_t mx_product_fp8(int prec, const MxProductArgs &a, hipStream_t st);
 
-// Sets on 4-bit rows: biases[l * k] = -||s||^2 / 2 of every slot's row
-// (-FLT_MAX: empty or invalid), and partials as launch_mfma writes them, G =
-// mx_sets_parts(n, d) rows of lpad.
-int64_t mx_sets_parts(int64_t n, int64_t d);
+// Sets on 4-bit rows: partials as launch_mfma writes them, mx_sets_parts(n)
+// rows of lpad (a multiple of kMxSets), with mx_sets_work(d, k) bytes of work
+// per kMxSets sets.
+int64_t mx_sets_parts(int64_t n);
+int64_t mx_sets_work(int64_t d, int64_t k);
 hipError_t launch_mx_sets(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets, int64_t l,
-                          int64_t k, float *biases, float *partials, int64_t lpad, hipStream_t st);
+                          int64_t k, void *work, float *partials, int64_t lpad, hipStream_t st);
 
 }  // namespace exemcl

@@ -1,11 +1,6 @@
-// kernels_mx_sets.hip -- f(S) = (2/n) sum_v max(0, max_s <v, s> - |s|^2 / 2) on
-// 4-bit rows: the clamp form of mfma_kernels.hpp on the 4-bit matrix cores,
-// whose sums of products are exact in fp32.
-#include <float.h>
-
-#include "internal.h"
-#include "mfma_kernels.hpp"
-#include "mx_device.hpp"
+// kernels_mx_sets.hip -- sets on 4-bit rows: the choice of a kernel, and the one
+// for long rows.
+#include "mx_sets.hpp"
 
 namespace exemcl {
 
@@ -40,9 +35,8 @@ __global__ __launch_bounds__(256) void mx_bias_kernel(const uint8_t *__restrict_
     if (lane == 0) biases[i] = (float)(-0.5 * q);
 }
 
-// 32 points x 16 sets per wavefront, operands from memory.
-constexpr int kSetRows = 32;
-
+// Rows too long for registers: 32 points x 16 sets per wavefront, operands
+// from memory.
 __global__ __launch_bounds__(256) void mx_sets_direct_kernel(const uint8_t *__restrict__ codes,
                                                              const uint8_t *__restrict__ scales, int64_t n, int64_t d,
                                                              const int32_t *__restrict__ sets, int64_t l, int64_t k,
@@ -53,7 +47,7 @@ __global__ __launch_bounds__(256) void mx_sets_direct_kernel(const uint8_t *__re
     if (part >= parts) return;
     const int64_t rb = mx_row_bytes(d, 4), rs = mx_row_scales(d);
     const int ksteps = (int)(mx_padded(d) / kMxRow);
-    const int64_t r0 = min(part * kSetRows + lr, n - 1), r1 = min(part * kSetRows + 16 + lr, n - 1);
+    const int64_t r0 = min(part * kMxSetRows + lr, n - 1), r1 = min(part * kMxSetRows + 16 + lr, n - 1);
     const int64_t j = grp * 16 + lr;
     f32x4 m0 = {0.0f, 0.0f, 0.0f, 0.0f}, m1 = m0;
     for (int64_t p = 0; p < k; ++p) {
@@ -77,29 +71,47 @@ __global__ __launch_bounds__(256) void mx_sets_direct_kernel(const uint8_t *__re
     float t = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (part * kSetRows + 4 * g + i < n) t += m0[i];
-        if (part * kSetRows + 16 + 4 * g + i < n) t += m1[i];
+        if (part * kMxSetRows + 4 * g + i < n) t += m0[i];
+        if (part * kMxSetRows + 16 + 4 * g + i < n) t += m1[i];
     }
     t += __shfl_xor(t, 16);
     t += __shfl_xor(t, 32);
     if (g == 0) partials[part * lpad + j] = t;
 }
 
+hipError_t run_long(const MxSetsArgs &x, hipStream_t st) {
+    const int64_t slots = x.l * x.k, groups = x.lpad / 16, parts = mx_sets_parts(x.n);
+    hipLaunchKernelGGL(mx_bias_kernel, flat_grid((slots + 3) / 4, 256), dim3(256), 0, st, x.codes, x.scales, x.n, x.d, x.sets,
+                       slots, (float *)x.work);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(mx_sets_direct_kernel, flat_grid((parts * groups + 3) / 4, 256), dim3(256), 0, st, x.codes, x.scales,
+                       x.n, x.d, x.sets, x.l, x.k, (const float *)x.work, parts, groups, x.partials, x.lpad);
+    return hipGetLastError();
+}
+
+// Fragments per row: the next of the compiled numbers.
+int mx_sets_bucket(int64_t d) {
+    const int ksteps = (int)(mx_padded(d) / kMxRow);
+    return ksteps <= 6 ? ksteps : (ksteps + 1) / 2 * 2;
+}
+
 }  // namespace
 
-int64_t mx_sets_parts(int64_t n, int64_t d) { return (n + kSetRows - 1) / kSetRows; }
+int64_t mx_sets_parts(int64_t n) { return (n + kMxSetRows - 1) / kMxSetRows; }
+
+int64_t mx_sets_work(int64_t d, int64_t k) {
+    if (d > kMxSetsD) return kMxSets * k * 4;
+    const int ks = mx_sets_bucket(d);
+    return (k + 1) / 2 * 2 * (ks * 1024 + (ks + 3) / 4 * 256 + 64);
+}
 
 hipError_t launch_mx_sets(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets, int64_t l,
-                          int64_t k, float *biases, float *partials, int64_t lpad, hipStream_t st) {
-    const int64_t slots = l * k, groups = lpad / 16, parts = mx_sets_parts(n, d);
-    hipLaunchKernelGGL(mx_bias_kernel, flat_grid((slots + 3) / 4, 256), dim3(256), 0, st, (const uint8_t *)codes,
-                       (const uint8_t *)scales, n, d, sets, slots, biases);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(mx_sets_direct_kernel, flat_grid((parts * groups + 3) / 4, 256), dim3(256), 0, st,
-                       (const uint8_t *)codes, (const uint8_t *)scales, n, d, sets, l, k, biases, parts, groups, partials,
-                       lpad);
-    return hipGetLastError();
+                          int64_t k, void *work, float *partials, int64_t lpad, hipStream_t st) {
+    const MxSetsArgs x{(const uint8_t *)codes, (const uint8_t *)scales, n, d, sets, l, k, (uint8_t *)work, partials, lpad};
+    if (d > kMxSetsD) return run_long(x, st);
+    const int ks = mx_sets_bucket(d);
+    return ks <= 6 ? mx_sets_short(ks, x, st) : mx_sets_wide(ks, x, st);
 }
 
 }  // namespace exemcl

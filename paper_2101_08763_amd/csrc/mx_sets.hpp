@@ -1,0 +1,294 @@
+// mx_sets.hpp -- f(S) = (2/n) sum_v max(0, max_s <v, s> - |s|^2 / 2) on 4-bit
+// rows: the clamp form of mfma_kernels.hpp on the 4-bit matrix cores, whose
+// sums of products are exact in fp32 (instantiated in kernels_mx_sets_*.hip).
+//
+// A workgroup keeps WAVES x RT x 16 points in registers (4 of them hold 16
+// points x 128 coordinates, a quarter of what 16-bit rows take) and the set
+// members stream past them through LDS: a tile is one member of each of 16
+// sets, two tiles a unit, UPS units a stage, three stages in flight.  A lane's
+// column is one set, so the maximum over its members stays in a register until
+// the set group ends.  Rows past n read as zeros and add nothing, a bias being
+// at most 0.  A sum of every 32 points is written, in the same order whatever
+// RT and WAVES are, so these follow the launch and not the result.
+#pragma once
+
+#include <float.h>
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+#include <utility>
+
+#include "internal.h"
+#include "mfma_kernels.hpp"
+#include "mx_device.hpp"
+
+namespace exemcl {
+
+constexpr int kMxSetRows = 32;        // points per partial sum
+constexpr int64_t kMxSetsD = 2048;    // longest rows kept in registers
+
+// Arguments of one launch: tiles (or biases) go to `work`.
+struct MxSetsArgs {
+    const uint8_t *codes, *scales;
+    int64_t n, d;
+    const int32_t *sets;
+    int64_t l, k;
+    uint8_t *work;
+    float *partials;
+    int64_t lpad;
+};
+
+hipError_t mx_sets_short(int ks, const MxSetsArgs &x, hipStream_t st);
+hipError_t mx_sets_wide(int ks, const MxSetsArgs &x, hipStream_t st);
+
+// A tile: KS fragments of 1 KiB in operand order, per 4 of them the scales of
+// every lane (byte b: of fragment 4 q + b), and 16 biases -|s|^2 / 2 (-FLT_MAX:
+// no member).
+template <int KS>
+struct MxTile {
+    static constexpr int SCALES = KS * 1024, BIAS = SCALES + (KS + 3) / 4 * 256, BYTES = BIAS + 64;
+};
+
+template <typename F, int... I>
+__device__ __forceinline__ void each_step(F f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+
+template <int KS, int RT, int WAVES>
+struct MxSetsPlan {
+    static constexpr int UNIT = 2 * MxTile<KS>::BYTES, THREADS = WAVES * 64;
+    static constexpr int UPS = UNIT >= 16384 ? 1 : 16384 / UNIT;            // units per stage
+    static constexpr int STAGE = UPS * UNIT;
+    static constexpr int LOADS = (STAGE + THREADS * 16 - 1) / (THREADS * 16);  // per thread
+    static constexpr int BUF = LOADS * THREADS * 16, LDS = 3 * BUF;
+    static constexpr int ROWS = WAVES * RT * 16;
+    static_assert(LDS <= kLdsBytes && RT % 2 == 0, "geometry");
+};
+
+template <int KS, int RT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *__restrict__ codes,
+                                                                const uint8_t *__restrict__ scales, int64_t n, int ksteps,
+                                                                const uint8_t *__restrict__ tiles, int members,
+                                                                int ngroups, int gpc, int nrb,
+                                                                float *__restrict__ partials, int64_t lpad) {
+    using P = MxSetsPlan<KS, RT, WAVES>;
+    using T = MxTile<KS>;
+    const int64_t parts = (n + kMxSetRows - 1) / kMxSetRows;
+    constexpr int SR = (KS + 3) / 4;  // scale registers of a row tile
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t b = flat_block(), chunk = b / nrb;
+    const int rb = (int)(b - chunk * nrb);
+    const int64_t g0 = chunk * gpc;
+    if (g0 >= ngroups) return;
+    const int groups = (int)min((int64_t)gpc, ngroups - g0), pairs = (members + 1) / 2, units = groups * pairs;
+
+    const uint8_t *stream = tiles + g0 * pairs * (int64_t)P::UNIT;
+    const int stages = (units + P::UPS - 1) / P::UPS;
+    auto issue = [&](int st) {
+        const int64_t at = (int64_t)st * P::STAGE, left = (int64_t)units * P::UNIT - at;
+        const auto win = window_rsrc(stream + at, (uint32_t)max((int64_t)0, min((int64_t)P::STAGE, left)));
+        unsigned char *buf = smem + st % 3 * P::BUF;
+#pragma unroll
+        for (int i = 0; i < P::LOADS; ++i)
+            window_to_lds16(win, buf + (i * P::THREADS + wave * 64) * 16, (uint32_t)((i * P::THREADS + tid) * 16));
+    };
+    issue(0);
+    issue(1);
+
+    // The points, and their scales as the tiles have theirs.
+    const int row_bytes = ksteps * 64, row_scales = ksteps * 4;
+    const int64_t row0 = (int64_t)rb * P::ROWS, rows = min((int64_t)P::ROWS, n - row0);
+    const auto vwin = window_rsrc(codes + row0 * row_bytes, (uint32_t)(rows * row_bytes));
+    const auto swin = window_rsrc(scales + row0 * row_scales, (uint32_t)(rows * row_scales));
+    i32x4 a[RT][KS];
+    int as[RT][SR];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = (wave * RT + rt) * 16 + lr;
+        uint32_t w[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            a[rt][ks] = window_load16<i32x4>(vwin, ks < ksteps ? (uint32_t)(row * row_bytes + ks * 64 + g * 16) : kDeadOffset);
+            w[ks] = __float_as_uint(window_load4(swin, ks < ksteps ? (uint32_t)(row * row_scales + ks * 4) : kDeadOffset));
+        }
+#pragma unroll
+        for (int q = 0; q < SR; ++q) as[rt][q] = 0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) as[rt][ks / 4] |= (int)((w[ks] >> (8 * g) & 255u) << (8 * (ks % 4)));
+    }
+
+    f32x4 m[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) m[rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};  // e0
+
+    auto tile = [&](const unsigned char *t, f32x4(&acc)[RT]) {
+        const float bias = *reinterpret_cast<const float *>(t + T::BIAS + lr * 4);
+        int bs[SR];
+#pragma unroll
+        for (int q = 0; q < SR; ++q) bs[q] = *reinterpret_cast<const int *>(t + T::SCALES + q * 256 + lane * 4);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[rt] = f32x4{bias, bias, bias, bias};
+        auto step = [&](auto kc) {
+            constexpr int ks = decltype(kc)::value;
+            const i32x4 x = *reinterpret_cast<const i32x4 *>(t + ks * 1024 + lane * 16);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                acc[rt] = mx_mma<ks % 4, ks % 4>(a[rt][ks], x, acc[rt], as[rt][ks / 4], bs[ks / 4]);
+        };
+        each_step(step, std::make_integer_sequence<int, KS>{});
+    };
+
+    int q = 0;
+    int64_t grp = g0;
+    for (int st = 0; st < stages; ++st) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P::LOADS) : "memory");
+        __syncthreads();
+        issue(st + 2);
+        const unsigned char *buf = smem + st % 3 * P::BUF;
+        const int last = min(P::UPS, units - st * P::UPS);
+        for (int u = 0; u < last; ++u) {
+            const unsigned char *t = buf + u * P::UNIT;
+            f32x4 x[RT], y[RT];
+            tile(t, x);
+            if (2 * q + 1 < members) {
+                tile(t + T::BYTES, y);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m[rt][i] = fmaxf(fmaxf(m[rt][i], x[rt][i]), y[rt][i]);
+            } else {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m[rt][i] = fmaxf(m[rt][i], x[rt][i]);
+            }
+            if (++q == pairs) {
+#pragma unroll
+                for (int i = 0; i < RT / 2; ++i) {
+                    const f32x4 u = m[2 * i] + m[2 * i + 1];
+                    float s = (u[0] + u[2]) + (u[1] + u[3]);
+                    s += __shfl_xor(s, 16);
+                    s += __shfl_xor(s, 32);
+                    const int64_t part = (row0 + wave * RT * 16) / kMxSetRows + i;
+                    if (g == 0 && part < parts) partials[part * lpad + grp * 16 + lr] = s;
+                    m[2 * i] = m[2 * i + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+                q = 0;
+                ++grp;
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
+}
+
+// Tile (group, member) of l sets of k members, one wavefront each; |s|^2 in 64
+// bits (the squares of a block's elements add up to a whole number of
+// quarters).  Slots behind the last member are copies of nothing.
+template <int KS>
+__global__ __launch_bounds__(256) void mx_sets_pack_kernel(const uint8_t *__restrict__ codes,
+                                                           const uint8_t *__restrict__ scales, int64_t n, int ksteps,
+                                                           const int32_t *__restrict__ sets, int64_t l, int k,
+                                                           int64_t ntiles, uint8_t *__restrict__ tiles) {
+    using T = MxTile<KS>;
+    const int64_t i = flat_block() * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, lr = lane & 15, g = lane >> 4;
+    if (i >= ntiles) return;
+    const int slots = (k + 1) / 2 * 2;
+    const int64_t grp = i / slots, j = grp * 16 + lr;
+    const int p = (int)(i - grp * slots);
+    if (p >= k) return;
+    const int64_t s = sets[min(j, l - 1) * k + p];
+    const bool live = j < l && s >= 0 && s < n;
+    const int64_t row = live ? s : 0;
+    uint8_t *t = tiles + i * T::BYTES;
+    double q = 0.0;
+#pragma unroll
+    for (int r = 0; r < (KS + 3) / 4; ++r) {
+        uint32_t packed = 0;
+#pragma unroll
+        for (int ks = r * 4; ks < KS && ks < r * 4 + 4; ++ks) {
+            i32x4 x = {0, 0, 0, 0};
+            uint32_t sc = 0;
+            if (live && ks < ksteps) {
+                x = *reinterpret_cast<const i32x4 *>(codes + row * (ksteps * 64) + ks * 64 + g * 16);
+                sc = scales[row * (ksteps * 4) + ks * 4 + g];
+            }
+            *reinterpret_cast<i32x4 *>(t + ks * 1024 + lane * 16) = x;
+            packed |= sc << (8 * (ks % 4));
+            float e = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float v[8];
+                mx_decode8<4>(u32x2{(uint32_t)x[c], 0}, v);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) e = fmaf(v[u], v[u], e);
+            }
+            const double f = mx_factor(sc);
+            q += (double)e * f * f;
+        }
+        *reinterpret_cast<uint32_t *>(t + T::SCALES + r * 256 + lane * 4) = packed;
+    }
+    q += __shfl_xor(q, 16);
+    q += __shfl_xor(q, 32);
+    if (g == 0) *reinterpret_cast<float *>(t + T::BIAS + lr * 4) = live ? (float)(-0.5 * q) : -FLT_MAX;
+}
+
+// How a launch splits its work: set groups per workgroup, chosen by rounds of
+// workgroups over the CUs, times a group's instructions and what a workgroup
+// starts with (its points, the first stages: about 4 000 clocks).
+template <int KS, int RT, int WAVES>
+double mx_sets_cost(const MxSetsArgs &x, int64_t groups, int64_t *gpc) {
+    using P = MxSetsPlan<KS, RT, WAVES>;
+    const int64_t nrb = (x.n + P::ROWS - 1) / P::ROWS;
+    const int64_t resident = std::max<int64_t>(1, device_cu_count()) * std::min(WAVES <= 4 ? 4 : 1, kLdsBytes / P::LDS);
+    const double group = (double)x.k * KS * RT * 16.0 * 2.0, start = 4000.0;
+    double best = 0.0;
+    for (int64_t c = 1; c <= groups; c = c < 16 ? c + 1 : c + c / 8) {
+        const int64_t wgs = nrb * ((groups + c - 1) / c), rounds = (wgs + resident - 1) / resident;
+        const double cost = (double)rounds * ((double)c * group + start);
+        if (c == 1 || cost < best) best = cost, *gpc = c;
+    }
+    return best;
+}
+
+template <int KS, int RT, int WAVES>
+hipError_t mx_sets_launch(const MxSetsArgs &x, int64_t groups, int64_t gpc, hipStream_t st) {
+    using P = MxSetsPlan<KS, RT, WAVES>;
+    auto kern = mx_sets_kernel<KS, RT, WAVES>;
+    static std::atomic<bool> ready[kMaxDevices];  // the attribute holds for one device
+    const int dev = current_device();
+    if (dev < 0) return hipErrorInvalidDevice;
+    if (!ready[dev].load(std::memory_order_acquire)) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
+        if (e != hipSuccess) return e;
+        ready[dev].store(true, std::memory_order_release);
+    }
+    const int64_t nrb = (x.n + P::ROWS - 1) / P::ROWS;
+    if (gpc * ((x.k + 1) / 2) > (1 << 30)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kern, flat_grid(nrb * ((groups + gpc - 1) / gpc), P::THREADS), dim3(P::THREADS), P::LDS, st, x.codes,
+                       x.scales, x.n, (int)(mx_padded(x.d) / kMxRow), x.work, (int)x.k, (int)groups, (int)gpc, (int)nrb,
+                       x.partials, x.lpad);
+    return hipGetLastError();
+}
+
+// Tiles, then the sums: wavefronts with RT row tiles where the points fill the
+// chip that way, small workgroups of two where they do not.
+template <int KS, int RT>
+hipError_t mx_sets_run(const MxSetsArgs &x, hipStream_t st) {
+    const int64_t groups = x.lpad / 16, slots = (x.k + 1) / 2 * 2, ntiles = groups * slots;
+    if (x.k > (1 << 24) || groups > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(mx_sets_pack_kernel<KS>, flat_grid((ntiles + 3) / 4, 256), dim3(256), 0, st, x.codes, x.scales, x.n,
+                       (int)(mx_padded(x.d) / kMxRow), x.sets, x.l, (int)x.k, ntiles, x.work);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    int64_t gpc = 1, gpc2 = 1;
+    // (two row tiles per fragment: LDS reads bound it, twice the time)
+    if (mx_sets_cost<KS, RT, 8>(x, groups, &gpc) <= 2.0 * mx_sets_cost<KS, 2, 4>(x, groups, &gpc2))
+        return mx_sets_launch<KS, RT, 8>(x, groups, gpc, st);
+    return mx_sets_launch<KS, 2, 4>(x, groups, gpc2, st);
+}
+
+}  // namespace exemcl
