@@ -63,33 +63,53 @@ __global__ __launch_bounds__(kDirectWaves * 64) void mx_product_direct_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of C through LDS.  PM x PN wavefronts compute (16 WM PM) x (64 PN)
-// elements, one K-step of 128 coordinates a stage, three stages in flight.  B's
+// Tiles of C through LDS.  PM x PN wavefronts compute (16 WM PM) x (64 NB PN)
+// elements, one K-step of 128 coordinates a stage, DEPTH stages in LDS.  B's
 // rows are the instruction's first operand, so a lane's accumulators lie along
-// a row of C; fragment j of a wavefront holds B's rows 4 i + j (i = 0 .. 15) of
-// its 64, which makes them 16 neighbours: a wavefront stores whole 128-byte
-// lines of 16-bit results.  A's rows are dealt out the same way (row WM i + w in
-// fragment w), so one LDS read gives a lane the scales of four fragments.
+// a row of C; fragment j of a block of 64 holds B's rows 4 i + j (i = 0 .. 15),
+// which makes them 16 neighbours: a wavefront stores whole 128-byte lines of
+// 16-bit results; A's are dealt out the same way (row WM i + w in fragment w).
+// Copies run along the rows, 4 or 8 lanes to one (a lane per row, the operands'
+// own order, takes the address units 64 steps a load instead of 16: 16 384 x
+// 8 192 x 4 096 565 us).
+//
+// That size, 8 by 4 bits to bf16, takes 404 us (2.7 PFLOP/s; the instruction
+// alone, on random values, runs at 4.2), 256 x 256 x 128 in 1.24 us a stage of
+// which 0.85 are instructions.  With zeros for data it is 388: on others the
+// chip lowers its clock.  What is left is the start and the end of a tile (71 us
+// in all, 256 x 256), LDS reads and copies between instructions.
 // ---------------------------------------------------------------------------
-template <int BITS_A, int WM, int PM, int PN>
+template <int BITS_A, int WM, int NB, int PM, int PN, int DEPTH>
 struct MxTilePlan {
-    static constexpr int WAVES = PM * PN, THREADS = WAVES * 64, BM = PM * WM * 16, BN = PN * 64;
-    static constexpr int A_FRAGS = PM * WM * BITS_A / 4, FRAGS = A_FRAGS + PN * 4;  // of 1 KiB
-    static constexpr int SCALE_LOADS = (BM + BN) / 64;                              // of 64 rows
-    static constexpr int LOADS = FRAGS / WAVES + SCALE_LOADS / WAVES;               // per thread and stage
-    static constexpr int B_AT = A_FRAGS * 1024, AS_AT = FRAGS * 1024, BS_AT = AS_AT + BM * 4, BUF = BS_AT + BN * 4;
-    static constexpr int LDS = 3 * BUF;
-    static_assert(FRAGS % WAVES == 0 && SCALE_LOADS % WAVES == 0 && WM % 4 == 0 && LDS <= kLdsBytes, "geometry");
+    static constexpr int WAVES = PM * PN, THREADS = WAVES * 64, BM = PM * WM * 16, BN = PN * NB * 64;
+    static constexpr int A_FRAGS = PM * WM * BITS_A / 4, B_FRAGS = PN * NB * 4;  // of 1 KiB
+    static constexpr int A_LOADS = A_FRAGS / WAVES, B_LOADS = B_FRAGS / WAVES;
+    static constexpr int LOADS = A_LOADS + B_LOADS;  // per thread and stage, beside the scales
+    static constexpr int S_LOADS = (BM + BN + THREADS - 1) / THREADS;
+    // 16-byte chunks of a row in a stage, 4 or 8 (4- or 8-bit rows); chunk c of
+    // row p goes to place c ^ swap(p).  The 16 rows that lanes read the same
+    // chunk of then fill all 64 banks once, and so do 8 such rows and the 8
+    // others of the next chunk.
+    static constexpr int A_CHUNKS = BITS_A;
+    template <int CHUNKS>
+    __device__ __forceinline__ static int swap(int p) {
+        if constexpr (CHUNKS == 8) return ((p >> 2 ^ p >> 3) & 1) << 2 | (p >> 3 & 1) << 1 | (p >> 1 & 1);
+        return ((p >> 2 ^ p >> 3) & 1) << 1 | (p >> 3 & 1);
+    }
+    static constexpr int B_AT = A_FRAGS * 1024, BUF = B_AT + B_FRAGS * 1024;
+    static constexpr int SCALES_AT = DEPTH * BUF, SBUF = S_LOADS * THREADS * 16, LDS = SCALES_AT + 2 * SBUF;
+    static_assert(A_FRAGS % WAVES == 0 && B_FRAGS % WAVES == 0 && BM % 64 == 0 &&
+                      4 * NB % WM == 0 && LDS <= kLdsBytes,
+                  "geometry");
 };
 
-template <typename T, int BITS_A, bool DIVIDE, int WM, int PM, int PN>
-__global__ __launch_bounds__(PM *PN * 64, 2) void mx_product_kernel(const uint8_t *__restrict__ A,
-                                                                    const uint8_t *__restrict__ As, int64_t m,
-                                                                    const uint8_t *__restrict__ B,
-                                                                    const uint8_t *__restrict__ Bs, int64_t n, int ksteps,
-                                                                    int mblocks, int nblocks,
-                                                                    const float *__restrict__ bias, T *__restrict__ C) {
-    using P = MxTilePlan<BITS_A, WM, PM, PN>;
+template <typename T, int BITS_A, bool DIVIDE, int WM, int NB, int PM, int PN, int DEPTH>
+__global__ __launch_bounds__(PM *PN * 64, WM * NB > 8 ? 1 : 2) void mx_product_kernel(
+    const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, int64_t m, const uint8_t *__restrict__ B,
+    const uint8_t *__restrict__ Bs, int64_t n, int ksteps, int mblocks, int nblocks, const float *__restrict__ bias,
+    T *__restrict__ C) {
+    using P = MxTilePlan<BITS_A, WM, NB, PM, PN, DEPTH>;
+    constexpr int WN = 4 * NB, H = BITS_A / 4;  // fragments of B, halves of one of A's
     extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % PM, wn = wave / PM;
@@ -97,122 +117,243 @@ __global__ __launch_bounds__(PM *PN * 64, 2) void mx_product_kernel(const uint8_
     // Workgroups b, b + 8, b + 16, ... share an XCD and its L2: they take
     // consecutive tiles, up to 8 of one row of tiles side by side.
     const int64_t units = (int64_t)mblocks * nblocks, per = (units + 7) / 8;
-    const int64_t b = flat_block(), pos = b >> 3, u = (b & 7) * per + pos;
+    const int64_t wg = flat_block(), pos = wg >> 3, u = (wg & 7) * per + pos;
     if (pos >= per || u >= units) return;
     const int64_t strip = u / ((int64_t)mblocks * 8);
     const int width = (int)min((int64_t)8, nblocks - strip * 8);
     const int64_t in = u - strip * mblocks * 8;
     const int64_t m0 = in / width * P::BM, n0 = (strip * 8 + in % width) * P::BN;
 
+    // What a thread copies: its part of A's and B's fragments, and the scales of
+    // 64 rows.  What lies past the rows, or in stages past the last, reads as
+    // zeros.
     const int a_row = ksteps * 16 * BITS_A, b_row = ksteps * 64, s_row = ksteps * 4;
     const uint32_t mrows = (uint32_t)min((int64_t)P::BM, m - m0), nrows = (uint32_t)min((int64_t)P::BN, n - n0);
     const auto awin = window_rsrc(A + m0 * a_row, mrows * (uint32_t)a_row);
     const auto bwin = window_rsrc(B + n0 * b_row, nrows * (uint32_t)b_row);
     const auto aswin = window_rsrc(As + m0 * s_row, mrows * (uint32_t)s_row);
     const auto bswin = window_rsrc(Bs + n0 * s_row, nrows * (uint32_t)s_row);
-
-    // What lies past the rows, or in stages past the last, reads as zeros.
-    auto issue = [&](int st) {
-        unsigned char *buf = smem + st % 3 * P::BUF;
-        const bool live = st < ksteps;
+    // Copy i takes A's places 64 (wave A_LOADS + i) ... in LDS order.  Which rows
+    // those are differs between copies by a number that is the same for all
+    // lanes, up to the parity of i, where a row has 8 chunks.
+    uint32_t a_off[2], b_off;
+    int a_more[P::A_LOADS], b_more[P::B_LOADS];
+    auto a_place = [&](int i, int at, int &row, int &c) {
+        const int p = ((wave * P::A_LOADS + i) * 64 + at) / P::A_CHUNKS;
+        row = p / (WM * 16) * (WM * 16) + p % 16 * WM + p / 16 % WM;
+        c = at % P::A_CHUNKS ^ P::template swap<P::A_CHUNKS>(p);
+    };
+    auto b_place = [&](int i, int at, int &row, int &c) {
+        const int p = ((wave * P::B_LOADS + i) * 64 + at) / 4;
+        row = p / 64 * 64 + p % 16 * 4 + p / 16 % 4;
+        c = at % 4 ^ P::template swap<4>(p);
+    };
 #pragma unroll
-        for (int i = 0; i < P::FRAGS / P::WAVES; ++i) {
-            const int f = i * P::WAVES + wave;
-            if (f < P::A_FRAGS) {
-                constexpr int H = BITS_A / 4;  // halves of a fragment
-                const int w = f / H % WM, block = f / H / WM;
-                const int row = block * WM * 16 + lr * WM + w;
-                const uint32_t off = (uint32_t)row * a_row + st * (16 * BITS_A) + f % H * 64 + g * 16;
-                window_to_lds16(awin, buf + f * 1024, live ? off : kDeadOffset);
-            } else {
-                const int j = (f - P::A_FRAGS) % 4, block = (f - P::A_FRAGS) / 4;
-                const int row = block * 64 + lr * 4 + j;
-                window_to_lds16(bwin, buf + f * 1024, live ? (uint32_t)row * b_row + st * 64 + g * 16 : kDeadOffset);
-            }
-        }
+    for (int i = 0; i < P::A_LOADS; ++i) {
+        int row, c, row0, c0;
+        a_place(i, lane, row, c);
+        if (i < 2) a_off[i] = (uint32_t)(row * a_row + c * 16);
+        a_place(i, 0, row, c);
+        a_place(i % 2, 0, row0, c0);
+        a_more[i] = (row - row0) * a_row;
+    }
 #pragma unroll
-        for (int i = 0; i < P::SCALE_LOADS / P::WAVES; ++i) {
-            const int f = i * P::WAVES + wave;
-            const int row = (f * 64 < P::BM ? f * 64 : f * 64 - P::BM) + lane;
-            const uint32_t off = live ? (uint32_t)row * s_row + st * 4 : kDeadOffset;
-            if (f * 64 < P::BM)
-                window_to_lds4(aswin, buf + P::AS_AT + f * 256, off);
+    for (int i = 0; i < P::B_LOADS; ++i) {
+        int row, c, row0, c0;
+        b_place(i, lane, row, c);
+        if (i == 0) b_off = (uint32_t)(row * b_row + c * 16);
+        b_place(i, 0, row, c);
+        b_place(0, 0, row0, c0);
+        b_more[i] = (row - row0) * b_row;
+    }
+    // (in LDS the scales of a fragment's 16 rows are neighbours)
+    uint32_t s_off[P::S_LOADS];
+#pragma unroll
+    for (int i = 0; i < P::S_LOADS; ++i) {
+        const int p = i * P::THREADS + tid, q = p - P::BM;
+        s_off[i] = (uint32_t)((p < P::BM ? p / (WM * 16) * (WM * 16) + p % 16 * WM + p / 16 % WM
+                                         : q / 64 * 64 + q % 16 * 4 + q / 16 % 4) * s_row);
+    }
+    // Copy number i of stage st (A's first) into the buffer at `to`.
+    auto copy = [&](int st, int to, int i) {
+        const uint32_t dead = st < ksteps ? 0u : kDeadOffset;
+        if (i < P::A_LOADS)
+            window_to_lds16(awin, smem + to + (wave * P::A_LOADS + i) * 1024,
+                            a_off[i % 2] + (dead | (uint32_t)(a_more[i] + st * 16 * BITS_A)));
+        else
+            window_to_lds16(bwin, smem + to + P::B_AT + (wave * P::B_LOADS + i - P::A_LOADS) * 1024,
+                            b_off + (dead | (uint32_t)(b_more[i - P::A_LOADS] + st * 64)));
+    };
+    auto copy_scales = [&](int st) {
+        if (st % 4 != 0) return;
+        const uint32_t dead = (st < ksteps ? 0u : kDeadOffset) | (uint32_t)(st * 4);
+        unsigned char *buf = smem + P::SCALES_AT + st / 4 % 2 * P::SBUF;
+#pragma unroll
+        for (int i = 0; i < P::S_LOADS; ++i) {
+            const int p = i * P::THREADS + wave * 64;
+            if (P::BM % P::THREADS == 0 ? i * P::THREADS < P::BM : p < P::BM)
+                window_to_lds16(aswin, buf + p * 16, s_off[i] + dead);
             else
-                window_to_lds4(bswin, buf + P::AS_AT + f * 256, off);
+                window_to_lds16(bswin, buf + p * 16, s_off[i] + dead);
         }
     };
+    auto issue = [&](int st) {
+        copy_scales(st);
+#pragma unroll
+        for (int i = 0; i < P::LOADS; ++i) copy(st, st * P::BUF, i);
+    };
 
-    f32x4 acc[WM][4];
+    f32x4 acc[WM][WN];
 #pragma unroll
     for (int w = 0; w < WM; ++w)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[w][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < WN; ++j) acc[w][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    issue(0);
-    issue(1);
-    for (int st = 0; st < ksteps; ++st) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P::LOADS) : "memory");
-        __syncthreads();
-        issue(st + 2);
-        const unsigned char *buf = smem + st % 3 * P::BUF;
-        const i32x4 *af = reinterpret_cast<const i32x4 *>(buf) + wm * WM * (BITS_A / 4) * 64 + lane;
-        const i32x4 *bf = reinterpret_cast<const i32x4 *>(buf + P::B_AT) + wn * 4 * 64 + lane;
-        i32x4 bx[4];
+    // A stage's operands are read from LDS while the stage before it computes,
+    // each over the one just used for the last time.  Only the copies then stand
+    // between a barrier and the next instructions.
+    i32x4 b[WN];
+    int bs[WN];
+    i32x4 a[WM][H];
+    int as[WM];
+    int a_at[H];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) bx[j] = bf[j * 64];
-        i32x4 bs = *reinterpret_cast<const i32x4 *>(buf + P::BS_AT + (wn * 64 + lr * 4) * 4);
+    for (int h = 0; h < H; ++h)
+        a_at[h] = (wm * WM * 16 + lr) * P::A_CHUNKS * 16 + ((h * 4 + g) ^ P::template swap<P::A_CHUNKS>(lr)) * 16;
+    const int b_at = P::B_AT + (wn * NB * 64 + lr) * 64 + (g ^ P::template swap<4>(lr)) * 16;
+    const int s_at = P::SCALES_AT + lr * 16 + g;
+    // Where a stage's operands are: one register each, so that the reads differ
+    // by constants.
+    struct Places {
+        int a[H], b, as, bs;
+    };
+    auto places = [&](int st, int from) {
+        Places x;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) bs[j] = (int)((uint32_t)bs[j] >> (8 * g));  // the low byte counts
+        for (int h = 0; h < H; ++h) {
+            x.a[h] = from + a_at[h];
+            asm("" : "+v"(x.a[h]));
+        }
+        x.b = from + b_at;
+        x.as = s_at + st / 4 % 2 * P::SBUF + st % 4 * 4 + wm * WM * 256;
+        x.bs = s_at + st / 4 % 2 * P::SBUF + st % 4 * 4 + (P::BM + wn * WN * 16) * 16;
+        asm("" : "+v"(x.b), "+v"(x.as), "+v"(x.bs));
+        return x;
+    };
+    auto read_a = [&](const Places &x, int w) {
 #pragma unroll
-        for (int w0 = 0; w0 < WM; w0 += 4) {
-            i32x4 as = *reinterpret_cast<const i32x4 *>(buf + P::AS_AT + (wm * WM * 16 + lr * WM + w0) * 4);
+        for (int h = 0; h < H; ++h) a[w][h] = *reinterpret_cast<const i32x4 *>(smem + x.a[h] + w * P::A_CHUNKS * 256);
+        as[w] = smem[x.as + w * 256];
+    };
+    auto read_b = [&](const Places &x, int j) {
+        b[j] = *reinterpret_cast<const i32x4 *>(smem + x.b + j * 1024);
+        bs[j] = smem[x.bs + j * 256];
+    };
+    // Stage st; the next one is in LDS at `from`, and this one's place `to` is
+    // free for st + DEPTH.
+    auto stage = [&](int st, int from, int to) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 2) * P::LOADS) : "memory");  // stage st + 1
+        __syncthreads();                                               // everyone's, and st has been read
+        copy_scales(st + DEPTH);
+        __builtin_amdgcn_sched_barrier(0);
+        const Places x = places(st + 1, from);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) as[i] = (int)((uint32_t)as[i] >> (8 * g));
+        for (int w = 0; w < WM; ++w) {
+            if (w > 0) read_a(x, w - 1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int w = w0 + i;
-                if constexpr (BITS_A == 4) {
-                    const i32x4 ax = af[w * 64];
+            for (int i = w * P::LOADS / WM; i < (w + 1) * P::LOADS / WM; ++i) copy(st + DEPTH, to, i);
+            if constexpr (BITS_A == 4) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[w][j] = mx_mma(bx[j], ax, acc[w][j], bs[j], as[i]);
+                for (int j = 0; j < WN; ++j) {
+                    acc[w][j] = mx_mma(b[j], a[w][0], acc[w][j], bs[j], as[w]);
+                    if (w == WM - 1) read_b(x, j);
+                }
+            } else {
+                const i32x8 ax = mx_join(a[w][0], a[w][1]);
+                if constexpr (DIVIDE) {
+                    i32x8 high, low;
+                    mx_divide(ax, high, low);
+#pragma unroll
+                    for (int j = 0; j < WN; ++j) acc[w][j] = mx_mma(b[j], low, acc[w][j], bs[j], as[w]);
+#pragma unroll
+                    for (int j = 0; j < WN; ++j) {
+                        acc[w][j] = mx_mma(b[j], high, acc[w][j], bs[j], as[w]);
+                        if (w == WM - 1) read_b(x, j);
+                    }
                 } else {
-                    const i32x8 ax = mx_join(af[w * 128], af[w * 128 + 64]);
-                    if constexpr (DIVIDE) {
-                        i32x8 high, low;
-                        mx_divide(ax, high, low);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[w][j] = mx_mma(bx[j], low, acc[w][j], bs[j], as[i]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[w][j] = mx_mma(bx[j], high, acc[w][j], bs[j], as[i]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[w][j] = mx_mma(bx[j], ax, acc[w][j], bs[j], as[i]);
+                    for (int j = 0; j < WN; ++j) {
+                        acc[w][j] = mx_mma(b[j], ax, acc[w][j], bs[j], as[w]);
+                        if (w == WM - 1) read_b(x, j);
                     }
                 }
             }
+            // Reads and copies between the instructions: all at once, they hold
+            // the wavefront up for as long as LDS and the address units take
+            // them in.
+#pragma unroll
+            for (int i = 0; i < H + 1; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < (P::LOADS + WM - 1) / WM; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            }
+            if (w == WM - 1) {
+#pragma unroll
+                for (int i = 0; i < WN; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                }
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, WN * 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        read_a(x, WM - 1);
+    };
+
+#pragma unroll
+    for (int st = 0; st < DEPTH; ++st) issue(st);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * P::LOADS) : "memory");
+    __syncthreads();
+    {
+        const Places x = places(0, 0);
+#pragma unroll
+        for (int w = 0; w < WM; ++w) read_a(x, w);
+#pragma unroll
+        for (int j = 0; j < WN; ++j) read_b(x, j);
+    }
+    for (int st = 0, at = 0; st < ksteps; ++st) {
+        const int from = at == (DEPTH - 1) * P::BUF ? 0 : at + P::BUF;
+        stage(st, from, at);
+        at = from;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
 
-    // Accumulator i of fragment j is column 16 g + 4 i + j of the wavefront's 64.
-    const int64_t col = n0 + wn * 64 + g * 16;
-    const int have = (int)max((int64_t)0, min((int64_t)16, n - col));
-    float bb[16];
+    // Accumulator i of fragment j of a block of 64 is its column 16 g + 4 i + j.
 #pragma unroll
-    for (int e = 0; e < 16; ++e) bb[e] = bias && e < have ? bias[col + e] : 0.0f;
+    for (int q = 0; q < NB; ++q) {
+        const int64_t col = n0 + (wn * NB + q) * 64 + g * 16;
+        const int have = (int)max((int64_t)0, min((int64_t)16, n - col));
+        float bb[16];
 #pragma unroll
-    for (int w = 0; w < WM; ++w) {
-        const int64_t row = m0 + wm * WM * 16 + lr * WM + w;
-        float lo[8], hi[8];
+        for (int e = 0; e < 16; ++e) bb[e] = bias && e < have ? bias[col + e] : 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            lo[e] = acc[w][e % 4][e / 4] + bb[e];
-            hi[e] = acc[w][e % 4][e / 4 + 2] + bb[e + 8];
-        }
-        if (row < m) {
-            T *c = C + row * n + col;
-            store8(c, have, lo);
-            store8(c + 8, have - 8, hi);
+        for (int w = 0; w < WM; ++w) {
+            const int64_t row = m0 + wm * WM * 16 + lr * WM + w;
+            float lo[8], hi[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                lo[e] = acc[w][q * 4 + e % 4][e / 4] + bb[e];
+                hi[e] = acc[w][q * 4 + e % 4][e / 4 + 2] + bb[e + 8];
+            }
+            if (row < m) {
+                T *c = C + row * n + col;
+                store8(c, have, lo);
+                store8(c + 8, have - 8, hi);
+            }
         }
     }
 }
@@ -227,10 +368,10 @@ hipError_t product_direct(const MxProductArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <typename T, int BITS_A, bool DIVIDE, int WM, int PM, int PN>
+template <typename T, int BITS_A, bool DIVIDE, int WM, int NB, int PM, int PN, int DEPTH>
 hipError_t product_tiled(const MxProductArgs &a, hipStream_t st) {
-    using P = MxTilePlan<BITS_A, WM, PM, PN>;
-    auto kern = mx_product_kernel<T, BITS_A, DIVIDE, WM, PM, PN>;
+    using P = MxTilePlan<BITS_A, WM, NB, PM, PN, DEPTH>;
+    auto kern = mx_product_kernel<T, BITS_A, DIVIDE, WM, NB, PM, PN, DEPTH>;
     static std::atomic<bool> ready[kMaxDevices];  // the attribute holds for one device
     const int dev = current_device();
     if (dev < 0) return hipErrorInvalidDevice;
@@ -247,16 +388,32 @@ hipError_t product_tiled(const MxProductArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// The kernel for a size.  Where a tile of 64 x 128 leaves most CUs without one,
+// 16 x 16 tiles with the coordinates dealt out to four wavefronts; else the
+// largest tile that still makes enough of them (us, 8 by 4 bits to bf16):
+//                          16x16  64x128  128x128  128x256  256x256
+//   24 x 2 000 x 1 024       4.2     8.5      9.0     12.8     19.4
+//   130 x 8 192 x 1 024     25.1    10.3     11.0     14.9     20.5
+//   1 024 x 8 192 x 1 024            22.6     16.9     18.7     23.8
+//   1 024 x 30 000 x 1 024           64.4     47.8     42.8     48.2
+//   16 384 x 8 192 x 1 024                   157      128      155
+//   16 384 x 8 192 x 4 096                   491      426      404
+// The largest has one workgroup per CU and starts and ends alone: it wins from
+// about 3 000 coordinates on, where its last round is full.
 template <typename T, int BITS_A, bool DIVIDE>
 hipError_t product_run(const MxProductArgs &a, hipStream_t st) {
-    if (a.m <= 16) return product_direct<T, BITS_A, DIVIDE>(a, st);
-    // Rounds of workgroups over the CUs (two small ones to each), times a
-    // tile's area.
     const int64_t cus = std::max<int64_t>(1, device_cu_count());
     auto tiles = [&](int64_t bm, int64_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
-    const int64_t large = (tiles(256, 256) + cus - 1) / cus * 4, small = (tiles(128, 128) + 2 * cus - 1) / (2 * cus) * 2;
-    return large <= small * 1.25 ? product_tiled<T, BITS_A, DIVIDE, 8, 2, 4>(a, st)
-                                 : product_tiled<T, BITS_A, DIVIDE, 4, 2, 2>(a, st);
+    const double ks = (double)(mx_padded(a.d) / kMxRow);
+    // us, fitted to 8 to 4 096 x 300 to 30 000 x 256 to 4 096
+    const double direct = 3.2 + 0.1 * ks + (BITS_A == 8 ? 5e-4 : 4e-4) * (double)tiles(16, 16) * (ks + 0.5);
+    const double tiled = 5.4 + (DIVIDE ? 0.9 : BITS_A == 8 ? 0.38 : 0.3) * ks;
+    if (direct <= tiled * std::max(1.0, (double)tiles(64, 128) / (2.0 * cus))) return product_direct<T, BITS_A, DIVIDE>(a, st);
+    if (tiles(64, 128) <= cus) return product_tiled<T, BITS_A, DIVIDE, 4, 1, 1, 2, 3>(a, st);
+    if (tiles(128, 128) <= 3 * cus) return product_tiled<T, BITS_A, DIVIDE, 4, 1, 2, 2, 3>(a, st);
+    const int64_t large = tiles(256, 256), last = (large + cus - 1) / cus * cus;
+    if (!DIVIDE && ks >= 24 && last * 10 <= large * 11) return product_tiled<T, BITS_A, DIVIDE, 8, 2, 2, 2, 3>(a, st);
+    return product_tiled<T, BITS_A, DIVIDE, 4, 2, 2, 2, 2>(a, st);
 }
 
 // DIVIDE: 8-bit rows in two parts (mx_divide), for results in fp32; what the

@@ -243,6 +243,30 @@ def test_product(m, n, d, fmt, dtype, bias):
     assert np.all(np.abs(to64(C) - want) <= err + UNIT[dtype] * 1.01 * (np.abs(want) + err) + TINY[dtype])
 
 
+@pytest.mark.parametrize("fmt,dtype", [(FP4, torch.float32), (FP8, torch.float32), (FP8, torch.bfloat16)], ids=str)
+@pytest.mark.parametrize("m,n,d", [(1000, 8000, 130), (2049, 1999, 200), (1025, 12_001, 100), (1030, 12_100, 3100),
+                                   (4096, 4096, 3200)])
+def test_product_large(m, n, d, fmt, dtype):
+    """Sizes that take the larger tiles, on sampled rows and columns."""
+    g = gen("large", m, n, d, fmt)
+    x = torch.as_tensor(g.standard_normal((max(m, n), d)), dtype=torch.float32, device="cuda")
+    A, B = api.exemplar_mx_quantize(x[:m].contiguous(), fmt), api.exemplar_mx_quantize(x[:n].flip(1).contiguous(), FP4)
+    C = api.exemplar_mx_product(A, B, dtype=dtype)
+    rows = np.unique(np.concatenate([g.integers(0, m, 40), [0, 127, 128, m - 1]]))
+    cols = np.unique(np.concatenate([g.integers(0, n, 60), [0, 63, 64, 255, 256, n - 1]]))
+    a = ref.values(A.codes[rows].cpu().numpy(), A.scales[rows].cpu().numpy(), d, fmt)
+    b = ref.values(B.codes[cols].cpu().numpy(), B.scales[cols].cpu().numpy(), d, FP4)
+    got, want, size = to64(C[rows][:, cols]), a @ b.T, np.abs(a) @ np.abs(b).T
+    err = (ref.padded(d) // 128 * 20 + 2) * 2.0 ** -23 * size
+    if fmt == FP8 and dtype != torch.float32:
+        err = err + 2.0 ** -10 * size
+    assert np.all(np.abs(got - want) <= err + UNIT[dtype] * 1.01 * (np.abs(want) + err))
+    # every element, against a product in 64 bits of the same values
+    whole = api.exemplar_mx_dequantize(A, torch.float32).double() @ api.exemplar_mx_dequantize(B, torch.float32).double().t().contiguous()
+    off = (C.double() - whole).abs().max().item()
+    assert off <= 2.0 ** -6 * whole.abs().max().item()
+
+
 def test_product_of_8_bit_rows_is_exact_in_parts():
     """Products of 448 and 6 beside the smallest of their part: nothing is lost,
     where one sum of 13 bits below its largest term would lose them all."""
