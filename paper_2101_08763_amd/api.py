@@ -298,26 +298,38 @@ class MxRows(NamedTuple):
     format: int
 
 
+_PRECISIONS: dict = {}  # precision_of, filled as types come
+
+
+def _precision(dtype) -> int:
+    p = _PRECISIONS.get(dtype)
+    if p is None:
+        p = _PRECISIONS[dtype] = precision_of(dtype)
+    return p
+
+
 def _mx_row(d: int, format: int):
     """(code bytes, scale bytes) of one stored row."""
-    if format not in (EXEMCL_MXFP4, EXEMCL_MXFP8):
+    if format != EXEMCL_MXFP4 and format != EXEMCL_MXFP8:
         raise ValueError("format must be EXEMCL_MXFP4 or EXEMCL_MXFP8")
     if not 1 <= d <= 1 << 22:
         raise ValueError("microscaled rows have 1 to 2^22 coordinates")
-    dp = (d + 127) // 128 * 128
-    return dp * format // 8, dp // 32
+    groups = (d + 127) // 128
+    return groups * 16 * format, groups * 4
 
 
 def _mx_check(q, name):
     """The rows of q, after its tensors' types and shapes were checked."""
     import torch
-    rb, rs = _mx_row(q.d, q.format)
-    for t, width in ((q.codes, rb), (q.scales, rs)):
-        if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[1] != width:
-            raise ValueError(f"{name}: codes must be uint8 n x {rb} and scales uint8 n x {rs}")
-    if q.codes.shape[0] != q.scales.shape[0]:
+    codes, scales, d, format = q
+    rb, rs = _mx_row(d, format)
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2 \
+            or codes.shape[1] != rb or scales.shape[1] != rs:
+        raise ValueError(f"{name}: codes must be uint8 n x {rb} and scales uint8 n x {rs}")
+    n = codes.shape[0]
+    if n != scales.shape[0]:
         raise ValueError(f"{name}: codes and scales have different numbers of rows")
-    return q.codes.shape[0]
+    return n
 
 
 def _mx_empty(n, d, format, device):
@@ -325,6 +337,31 @@ def _mx_empty(n, d, format, device):
     rb, rs = _mx_row(d, format)
     return MxRows(torch.empty((n, rb), dtype=torch.uint8, device=device),
                   torch.empty((n, rs), dtype=torch.uint8, device=device), d, format)
+
+
+def _run(name, tensors, stream, *args):
+    """Call ``name`` of the library on the device of ``tensors`` (the first
+    one's; None: not given) with ``args`` and the stream, and raise its error.
+    The checks and messages are _check_device's; the calls on rows can be a few
+    microseconds each, so the common case takes the short way."""
+    import torch
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (dev < 0 or t.get_device() != dev or not t.is_contiguous()):
+            _check_device(*tensors)
+    fn = getattr(_LIB or load(), name)
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _stream(stream))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, name)
+
+
+def _at(t):
+    """A tensor's address, for an argument that may be None."""
+    return None if t is None else t.data_ptr()
 
 
 def exemplar_mx_layout(d: int, format: int):
@@ -341,16 +378,15 @@ def exemplar_mx_quantize(x, format, out=None, stream=None):
     exemplar_mx_quantize in exemcl.h)."""
     if x.dim() != 2:
         raise ValueError("x must be n x d")
-    prec = precision_of(x.dtype)
+    prec = _precision(x.dtype)
     n, d = x.shape
     if out is None:
         out = _mx_empty(n, d, format, x.device)
     elif out.d != d or out.format != format or _mx_check(out, "out") != n:
         raise ValueError("out must be MxRows of x's shape and the format")
-    with _device_scope(_check_device(x, out.codes, out.scales)):
-        rc = load().exemplar_mx_quantize(_ptr(x), n, d, prec, format, _ptr(out.codes), _ptr(out.scales), _stream(stream))
-    if rc != EXEMCL_OK:
-        raise ExemclError(rc, "exemplar_mx_quantize")
+    codes, scales = out.codes, out.scales
+    _run("exemplar_mx_quantize", (x, codes, scales), stream, x.data_ptr(), n, d, prec, format, codes.data_ptr(),
+         scales.data_ptr())
     return out
 
 
@@ -358,17 +394,15 @@ def exemplar_mx_dequantize(q, dtype, out=None, stream=None):
     """The values of MxRows q as an n x d tensor of ``dtype`` (see
     exemplar_mx_dequantize in exemcl.h)."""
     import torch
-    prec = precision_of(dtype)
+    prec = _precision(dtype)
     n = _mx_check(q, "q")
+    codes, scales, d, format = q
     if out is None:
-        out = torch.empty((n, q.d), dtype=dtype, device=q.codes.device)
-    elif out.dtype != dtype or out.shape != (n, q.d):
+        out = torch.empty((n, d), dtype=dtype, device=codes.device)
+    elif out.dtype != dtype or out.shape != (n, d):
         raise ValueError("out must be an n x d tensor of the dtype")
-    with _device_scope(_check_device(q.codes, q.scales, out)):
-        rc = load().exemplar_mx_dequantize(_ptr(q.codes), _ptr(q.scales), n, q.d, q.format, prec, _ptr(out),
-                                           _stream(stream))
-    if rc != EXEMCL_OK:
-        raise ExemclError(rc, "exemplar_mx_dequantize")
+    _run("exemplar_mx_dequantize", (codes, scales, out), stream, codes.data_ptr(), scales.data_ptr(), n, d, format, prec,
+         out.data_ptr())
     return out
 
 
@@ -380,26 +414,23 @@ def exemplar_rmsnorm(x, weight=None, residual=None, eps=1e-6, format=None, strea
     import torch
     if x.dim() != 2:
         raise ValueError("x must be n x d")
-    prec = precision_of(x.dtype)
+    dtype, device = x.dtype, x.device
+    prec = _precision(dtype)
     n, d = x.shape
-    if weight is not None and (weight.dtype != x.dtype or weight.shape != (d,)):
+    if weight is not None and (weight.dtype != dtype or weight.shape != (d,)):
         raise ValueError("weight must have x's type and d elements")
-    if residual is not None and (residual.dtype != x.dtype or residual.shape != x.shape):
+    if residual is not None and (residual.dtype != dtype or residual.shape != x.shape):
         raise ValueError("residual must have x's type and shape")
-    h = x if residual is None else torch.empty_like(x, memory_format=torch.contiguous_format)
-    rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(n, dtype=torch.float32, device=device)
+    h = x if residual is None else torch.empty((n, d), dtype=dtype, device=device)
     if format is None or format == EXEMCL_MX_NONE:
-        y = torch.empty_like(x, memory_format=torch.contiguous_format)
-        codes, scales, fmt = y, None, EXEMCL_MX_NONE
+        y = codes = torch.empty((n, d), dtype=dtype, device=device)
+        scales, format = None, EXEMCL_MX_NONE
     else:
-        y = _mx_empty(n, d, format, x.device)
-        codes, scales, fmt = y.codes, y.scales, format
-    with _device_scope(_check_device(x, residual, weight, codes)):
-        rc = load().exemplar_rmsnorm(_ptr(x), _ptr(residual), _ptr(weight), n, d, prec, eps, fmt,
-                                     _ptr(None if residual is None else h), _ptr(codes), _ptr(scales), _ptr(rstd),
-                                     _stream(stream))
-    if rc != EXEMCL_OK:
-        raise ExemclError(rc, "exemplar_rmsnorm")
+        y = _mx_empty(n, d, format, device)
+        codes, scales = y.codes, y.scales
+    _run("exemplar_rmsnorm", (x, residual, weight), stream, x.data_ptr(), _at(residual), _at(weight), n, d, prec, eps,
+         format, None if residual is None else h.data_ptr(), codes.data_ptr(), _at(scales), rstd.data_ptr())
     return y, h, rstd
 
 
@@ -411,22 +442,20 @@ def exemplar_rmsnorm_backward(dy, h, weight, rstd, dh=None, stream=None):
     import torch
     if h.dim() != 2:
         raise ValueError("h must be n x d")
-    prec = precision_of(h.dtype)
+    dtype, device = h.dtype, h.device
+    prec = _precision(dtype)
     n, d = h.shape
     for t, name in ((dy, "dy"), (dh, "dh")):
-        if t is not None and (t.dtype != h.dtype or t.shape != h.shape):
+        if t is not None and (t.dtype != dtype or t.shape != h.shape):
             raise ValueError(f"{name} must have h's type and shape")
-    if weight is not None and (weight.dtype != h.dtype or weight.shape != (d,)):
+    if weight is not None and (weight.dtype != dtype or weight.shape != (d,)):
         raise ValueError("weight must have h's type and d elements")
     if rstd.dtype != torch.float32 or rstd.shape != (n,):
         raise ValueError("rstd must be float32 with n elements")
-    dx = torch.empty_like(h, memory_format=torch.contiguous_format)
-    dw = torch.empty(d, dtype=torch.float32, device=h.device)
-    with _device_scope(_check_device(h, dy, weight, rstd, dh)):
-        rc = load().exemplar_rmsnorm_backward(_ptr(dy), _ptr(h), _ptr(weight), _ptr(rstd), _ptr(dh), n, d, prec, _ptr(dx),
-                                              _ptr(dw), _stream(stream))
-    if rc != EXEMCL_OK:
-        raise ExemclError(rc, "exemplar_rmsnorm_backward")
+    dx = torch.empty((n, d), dtype=dtype, device=device)
+    dw = torch.empty(d, dtype=torch.float32, device=device)
+    _run("exemplar_rmsnorm_backward", (h, dy, weight, rstd, dh), stream, dy.data_ptr(), h.data_ptr(), _at(weight),
+         rstd.data_ptr(), _at(dh), n, d, prec, dx.data_ptr(), dw.data_ptr())
     return dx, dw
 
 
@@ -436,23 +465,22 @@ def exemplar_mx_product(A, B, bias=None, dtype=None, out=None, stream=None):
     exemplar_mx_product in exemcl.h)."""
     import torch
     dtype = torch.float32 if dtype is None else dtype
-    prec = precision_of(dtype)
+    prec = _precision(dtype)
     m, n = _mx_check(A, "A"), _mx_check(B, "B")
-    if A.d != B.d:
+    a, a_scales, d, format = A
+    b, b_scales = B.codes, B.scales
+    if d != B.d:
         raise ValueError("A and B must have the same number of coordinates")
     if B.format != EXEMCL_MXFP4:
         raise ValueError("B must be EXEMCL_MXFP4 rows")
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,)):
         raise ValueError("bias must be float32 with one element per row of B")
     if out is None:
-        out = torch.empty((m, n), dtype=dtype, device=A.codes.device)
+        out = torch.empty((m, n), dtype=dtype, device=a.device)
     elif out.dtype != dtype or out.shape != (m, n):
         raise ValueError("out must be an m x n tensor of the dtype")
-    with _device_scope(_check_device(A.codes, A.scales, B.codes, B.scales, bias, out)):
-        rc = load().exemplar_mx_product(_ptr(A.codes), _ptr(A.scales), m, A.format, _ptr(B.codes), _ptr(B.scales), n, A.d,
-                                        _ptr(bias), prec, _ptr(out), _stream(stream))
-    if rc != EXEMCL_OK:
-        raise ExemclError(rc, "exemplar_mx_product")
+    _run("exemplar_mx_product", (a, a_scales, b, b_scales, bias, out), stream, a.data_ptr(), a_scales.data_ptr(), m, format,
+         b.data_ptr(), b_scales.data_ptr(), n, d, _at(bias), prec, out.data_ptr())
     return out
 
 
@@ -461,7 +489,8 @@ def exemplar_mx_eval(V, sets, out=None, stream=None):
     ``sets`` (see exemplar_mx_eval in exemcl.h)."""
     import torch
     n = _mx_check(V, "V")
-    if V.format != EXEMCL_MXFP4:
+    codes, scales, d, format = V
+    if format != EXEMCL_MXFP4:
         raise ValueError("V must be EXEMCL_MXFP4 rows")
     if sets.dim() != 2:
         raise ValueError("sets must be l x k")
@@ -469,13 +498,11 @@ def exemplar_mx_eval(V, sets, out=None, stream=None):
         raise TypeError("sets must be int32")
     l, k = sets.shape
     if out is None:
-        out = torch.empty(l, dtype=torch.float32, device=V.codes.device)
+        out = torch.empty(l, dtype=torch.float32, device=codes.device)
     elif out.dtype != torch.float32 or out.numel() != l:
         raise ValueError("out must be float32 with l elements")
-    with _device_scope(_check_device(V.codes, V.scales, sets, out)):
-        rc = load().exemplar_mx_eval(_ptr(V.codes), _ptr(V.scales), n, V.d, _ptr(sets), l, k, _ptr(out), _stream(stream))
-    if rc != EXEMCL_OK:
-        raise ExemclError(rc, "exemplar_mx_eval")
+    _run("exemplar_mx_eval", (codes, scales, sets, out), stream, codes.data_ptr(), scales.data_ptr(), n, d, sets.data_ptr(),
+         l, k, out.data_ptr())
     return out
 
 

@@ -161,8 +161,9 @@ __global__ __launch_bounds__(norm_block(TPR)) void rmsnorm_kernel(const T *x, co
 // ---------------------------------------------------------------------------
 // Its gradient, from the saved v = h and rstd:  with xhat = h rstd and
 // g = dy w,  dx = rstd (g - xhat mean(g xhat)) + dh  and  dw = sum over rows
-// of dy xhat.  A thread keeps the same columns for all rows it sees, and
-// their part of dw in registers; a workgroup's parts are added in LDS in a
+// of dy xhat.  A thread keeps the same columns for all rows it sees, their
+// weights and their part of dw in registers, and loads a row while it works on
+// the one before; a workgroup's parts are added in LDS in a
 // fixed order and written as one row of `partial` (grid x d).
 // ---------------------------------------------------------------------------
 template <typename T, int TPR, int CPT>
@@ -170,45 +171,61 @@ __global__ __launch_bounds__(256) void rmsnorm_grad_kernel(const T *__restrict__
                                                            const T *__restrict__ w, const float *__restrict__ rstd_in,
                                                            const T *__restrict__ dh, int64_t n, int d,
                                                            T *__restrict__ dx, float *__restrict__ partial) {
+    using vec = typename Chunk<T>::vec;
     constexpr int RPB = 256 / TPR, COLS = TPR * CPT * 8;
     __shared__ float lds[8];
     __shared__ float sums[RPB > 1 ? RPB * COLS : 1];
     const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
     float dw[CPT][8] = {};
-    for (int64_t base = (int64_t)blockIdx.x * RPB; base < n; base += (int64_t)gridDim.x * RPB) {
-        const int64_t row = base + slot;
-        const bool live = row < n;
-        const int64_t at = (live ? row : n - 1) * d;
-        const float rstd = rstd_in[live ? row : n - 1];
-        float xh[CPT][8], g[CPT][8], s = 0.0f;
+    vec ww[CPT], nh[CPT], ng[CPT], no[CPT];
+    auto load = [&](int64_t row) {
+        const int64_t at = min(row, n - 1) * d;
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
             const int d0 = (t + i * TPR) * 8;
-            load8(h + at + d0, d - d0, xh[i]);
-            load8(dy + at + d0, d - d0, g[i]);
-            float ww[8];
-            if (w)
-                load8(w + d0, d - d0, ww);
-            else
+            nh[i] = load8(h + at + d0, d - d0);
+            ng[i] = load8(dy + at + d0, d - d0);
+            if (dh) no[i] = load8(dh + at + d0, d - d0);
+        }
+    };
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ww[e] = 1.0f;
+    for (int i = 0; i < CPT; ++i) {
+        const int d0 = (t + i * TPR) * 8;
+        if (w)
+            ww[i] = load8(w + d0, d - d0);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ww[i][e] = (T)1.0f;
+    }
+    load((int64_t)blockIdx.x * RPB + slot);
+    for (int64_t base = (int64_t)blockIdx.x * RPB; base < n; base += (int64_t)gridDim.x * RPB) {
+        const int64_t row = base + slot;
+        const bool live = row < n;
+        const float rstd = rstd_in[live ? row : n - 1];
+        vec ch[CPT], cg[CPT], co[CPT];
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) ch[i] = nh[i], cg[i] = ng[i], co[i] = no[i];
+        load(row + (int64_t)gridDim.x * RPB);  // the next row's, or the last one again
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < CPT; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                xh[i][e] *= rstd;
-                if (live) dw[i][e] = fmaf(g[i][e], xh[i][e], dw[i][e]);
-                g[i][e] *= ww[e];
-                s = fmaf(g[i][e], xh[i][e], s);
+                const float xh = to_f32((T)ch[i][e]) * rstd, g = to_f32((T)cg[i][e]);
+                if (live) dw[i][e] = fmaf(g, xh, dw[i][e]);
+                s = fmaf(g * to_f32((T)ww[i][e]), xh, s);
             }
-        }
         const float c = row_sum<TPR>(s, lds) / (float)d;
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
             const int d0 = (t + i * TPR) * 8;
-            float o[8] = {};
-            if (dh) load8(dh + at + d0, d - d0, o);
+            float o[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf(rstd, fmaf(-xh[i][e], c, g[i][e]), o[e]);
-            if (live) store8(dx + at + d0, d - d0, o);
+            for (int e = 0; e < 8; ++e) {
+                const float xh = to_f32((T)ch[i][e]) * rstd, g = to_f32((T)cg[i][e]) * to_f32((T)ww[i][e]);
+                o[e] = fmaf(rstd, fmaf(-xh, c, g), dh ? to_f32((T)co[i][e]) : 0.0f);
+            }
+            if (live) store8(dx + (row * d + d0), d - d0, o);
         }
     }
     if (!partial) return;
@@ -284,14 +301,20 @@ __global__ __launch_bounds__(256) void rmsnorm_dw_long_kernel(const T *__restric
 }
 
 // dw[c] = sum over g of partial[g][c], in 64 bits and a fixed order.
-constexpr int kDwCols = 32, kDwRows = 32;
+constexpr int kDwCols = 16, kDwRows = 64, kDwUnroll = 8;
 __global__ __launch_bounds__(kDwCols *kDwRows) void column_sum_kernel(const float *__restrict__ partial, int G, int d,
                                                                        float *__restrict__ dw) {
     __shared__ double part[kDwRows][kDwCols + 1];
     const int cl = threadIdx.x % kDwCols, q = threadIdx.x / kDwCols, c = blockIdx.x * kDwCols + cl;
     double s = 0.0;
     if (c < d)
-        for (int g = q; g < G; g += kDwRows) s += (double)partial[(int64_t)g * d + c];
+        for (int g = q; g < G; g += kDwRows * kDwUnroll) {
+            float x[kDwUnroll];
+#pragma unroll
+            for (int u = 0; u < kDwUnroll; ++u) x[u] = partial[(int64_t)min(g + u * kDwRows, G - 1) * d + c];
+#pragma unroll
+            for (int u = 0; u < kDwUnroll; ++u) s += g + u * kDwRows < G ? (double)x[u] : 0.0;
+        }
     part[q][cl] = s;
     __syncthreads();
 #pragma unroll
@@ -440,7 +463,7 @@ int64_t rmsnorm_grad_parts(int64_t n, int64_t d) {
     const int64_t chunks = (d + 7) / 8;
     if (chunks > 1024) return std::min<int64_t>(n, 64);
     const int64_t rpb = chunks <= 32 ? 16 : chunks <= 256 ? 4 : 1;
-    return std::min<int64_t>((n + rpb - 1) / rpb, 1024);
+    return std::min<int64_t>((n + rpb - 1) / rpb, 512);  // as many as are resident
 }
 
 hipError_t launch_rmsnorm_grad(int prec, const NormGradArgs &a, hipStream_t st) {

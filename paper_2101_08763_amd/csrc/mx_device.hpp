@@ -123,15 +123,19 @@ struct Chunk {
 };
 
 template <typename T>
+__device__ __forceinline__ typename Chunk<T>::vec load8(const T *p, int have) {
+    if (have >= 8) return *reinterpret_cast<const typename Chunk<T>::vec *>(p);
+    typename Chunk<T>::vec x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < have ? p[i] : (T)0.0f;
+    return x;
+}
+
+template <typename T>
 __device__ __forceinline__ void load8(const T *p, int have, float (&v)[8]) {
-    if (have >= 8) {
-        const auto x = *reinterpret_cast<const typename Chunk<T>::vec *>(p);
+    const auto x = load8(p, have);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f32((T)x[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < have ? to_f32(p[i]) : 0.0f;
-    }
+    for (int i = 0; i < 8; ++i) v[i] = to_f32((T)x[i]);
 }
 
 template <typename T>

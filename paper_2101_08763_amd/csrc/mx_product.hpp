@@ -66,9 +66,10 @@ __global__ __launch_bounds__(kDirectWaves * 64) void mx_product_direct_kernel(
 // Tiles of C through LDS.  PM x PN wavefronts compute (16 WM PM) x (64 NB PN)
 // elements, one K-step of 128 coordinates a stage, DEPTH stages in LDS.  B's
 // rows are the instruction's first operand, so a lane's accumulators lie along
-// a row of C; fragment j of a block of 64 holds B's rows 4 i + j (i = 0 .. 15),
-// which makes them 16 neighbours: a wavefront stores whole 128-byte lines of
-// 16-bit results; A's are dealt out the same way (row WM i + w in fragment w).
+// a row of C, 16 bytes of fp32 results.  For 16-bit ones fragment j of a block of
+// 64 holds B's rows 4 i + j (i = 0 .. 15), which makes them 16 neighbours and a
+// wavefront's stores whole 128-byte lines; A's are dealt out the same way (row
+// WM i + w in fragment w).
 // Copies run along the rows, 4 or 8 lanes to one (a lane per row, the operands'
 // own order, takes the address units 64 steps a load instead of 16: 16 384 x
 // 8 192 x 4 096 565 us).
@@ -136,6 +137,7 @@ __global__ __launch_bounds__(PM *PN * 64, WM * NB > 8 ? 1 : 2) void mx_product_k
     // Copy i takes A's places 64 (wave A_LOADS + i) ... in LDS order.  Which rows
     // those are differs between copies by a number that is the same for all
     // lanes, up to the parity of i, where a row has 8 chunks.
+    auto b_row_at = [](int p) { return sizeof(T) == 4 ? p : p / 64 * 64 + p % 16 * 4 + p / 16 % 4; };
     uint32_t a_off[2], b_off;
     int a_more[P::A_LOADS], b_more[P::B_LOADS];
     auto a_place = [&](int i, int at, int &row, int &c) {
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(PM *PN * 64, WM * NB > 8 ? 1 : 2) void mx_product_k
     };
     auto b_place = [&](int i, int at, int &row, int &c) {
         const int p = ((wave * P::B_LOADS + i) * 64 + at) / 4;
-        row = p / 64 * 64 + p % 16 * 4 + p / 16 % 4;
+        row = b_row_at(p);
         c = at % 4 ^ P::template swap<4>(p);
     };
 #pragma unroll
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(PM *PN * 64, WM * NB > 8 ? 1 : 2) void mx_product_k
     for (int i = 0; i < P::S_LOADS; ++i) {
         const int p = i * P::THREADS + tid, q = p - P::BM;
         s_off[i] = (uint32_t)((p < P::BM ? p / (WM * 16) * (WM * 16) + p % 16 * WM + p / 16 % WM
-                                         : q / 64 * 64 + q % 16 * 4 + q / 16 % 4) * s_row);
+                                         : b_row_at(q)) * s_row);
     }
     // Copy number i of stage st (A's first) into the buffer at `to`.
     auto copy = [&](int st, int to, int i) {
@@ -332,27 +334,55 @@ __global__ __launch_bounds__(PM *PN * 64, WM * NB > 8 ? 1 : 2) void mx_product_k
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
 
-    // Accumulator i of fragment j of a block of 64 is its column 16 g + 4 i + j.
+    // Accumulator i of fragment j of a block of 64 is its column 16 g + 4 i + j;
+    // with 32-bit results 16 j + 4 g + i.
 #pragma unroll
     for (int q = 0; q < NB; ++q) {
-        const int64_t col = n0 + (wn * NB + q) * 64 + g * 16;
-        const int have = (int)max((int64_t)0, min((int64_t)16, n - col));
-        float bb[16];
+        const int64_t block = n0 + (wn * NB + q) * 64;
+        if constexpr (sizeof(T) == 4) {
+            typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-        for (int e = 0; e < 16; ++e) bb[e] = bias && e < have ? bias[col + e] : 0.0f;
+            for (int j = 0; j < 4; ++j) {
+                const int64_t col = block + j * 16 + g * 4;
+                const int have = (int)max((int64_t)0, min((int64_t)4, n - col));
+                f32x4 bb;
 #pragma unroll
-        for (int w = 0; w < WM; ++w) {
-            const int64_t row = m0 + wm * WM * 16 + lr * WM + w;
-            float lo[8], hi[8];
+                for (int e = 0; e < 4; ++e) bb[e] = bias && e < have ? bias[col + e] : 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                lo[e] = acc[w][q * 4 + e % 4][e / 4] + bb[e];
-                hi[e] = acc[w][q * 4 + e % 4][e / 4 + 2] + bb[e + 8];
+                for (int w = 0; w < WM; ++w) {
+                    const int64_t row = m0 + wm * WM * 16 + lr * WM + w;
+                    const f32x4 v = acc[w][q * 4 + j] + bb;
+                    if (row >= m) continue;
+                    float *c = (float *)C + row * n + col;
+                    if (have == 4) {
+                        *reinterpret_cast<vec *>(c) = v;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (e < have) c[e] = v[e];
+                    }
+                }
             }
-            if (row < m) {
-                T *c = C + row * n + col;
-                store8(c, have, lo);
-                store8(c + 8, have - 8, hi);
+        } else {
+            const int64_t col = block + g * 16;
+            const int have = (int)max((int64_t)0, min((int64_t)16, n - col));
+            float bb[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) bb[e] = bias && e < have ? bias[col + e] : 0.0f;
+#pragma unroll
+            for (int w = 0; w < WM; ++w) {
+                const int64_t row = m0 + wm * WM * 16 + lr * WM + w;
+                float lo[8], hi[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    lo[e] = acc[w][q * 4 + e % 4][e / 4] + bb[e];
+                    hi[e] = acc[w][q * 4 + e % 4][e / 4 + 2] + bb[e + 8];
+                }
+                if (row < m) {
+                    T *c = C + row * n + col;
+                    store8(c, have, lo);
+                    store8(c + 8, have - 8, hi);
+                }
             }
         }
     }

@@ -184,56 +184,73 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
 }
 
-// Tile (group, member) of l sets of k members, one wavefront each; |s|^2 in 64
-// bits (the squares of a block's elements add up to a whole number of
-// quarters).  Slots behind the last member are copies of nothing.
+// Tile (group, member) of l sets of k members, WPT wavefronts each, which take
+// turns of four fragments; |s|^2 in 64 bits (the squares of a block's elements
+// add up to a whole number of quarters).  Slots behind the last member are left
+// alone.
+constexpr int mx_pack_waves(int ks) { return ks <= 4 ? 1 : ks <= 8 ? 2 : 4; }
+
 template <int KS>
 __global__ __launch_bounds__(256) void mx_sets_pack_kernel(const uint8_t *__restrict__ codes,
                                                            const uint8_t *__restrict__ scales, int64_t n, int ksteps,
                                                            const int32_t *__restrict__ sets, int64_t l, int k,
                                                            int64_t ntiles, uint8_t *__restrict__ tiles) {
     using T = MxTile<KS>;
-    const int64_t i = flat_block() * 4 + (threadIdx.x >> 6);
+    constexpr int WPT = mx_pack_waves(KS), TILES = 4 / WPT;
+    __shared__ double part[4][16];
+    const int wave = threadIdx.x >> 6, turn = wave % WPT;
+    const int64_t i = flat_block() * TILES + wave / WPT;
     const int lane = threadIdx.x & 63, lr = lane & 15, g = lane >> 4;
-    if (i >= ntiles) return;
     const int slots = (k + 1) / 2 * 2;
     const int64_t grp = i / slots, j = grp * 16 + lr;
     const int p = (int)(i - grp * slots);
-    if (p >= k) return;
-    const int64_t s = sets[min(j, l - 1) * k + p];
-    const bool live = j < l && s >= 0 && s < n;
+    const bool there = i < ntiles && p < k;
+    const int64_t s = there ? sets[min(j, l - 1) * k + p] : -1;
+    const bool live = there && j < l && s >= 0 && s < n;
     const int64_t row = live ? s : 0;
     uint8_t *t = tiles + i * T::BYTES;
     double q = 0.0;
+    if (there) {
 #pragma unroll
-    for (int r = 0; r < (KS + 3) / 4; ++r) {
-        uint32_t packed = 0;
+        for (int r0 = 0; r0 < (KS + 3) / 4; r0 += WPT) {
+            const int r = r0 + turn;
+            uint32_t packed = 0;
 #pragma unroll
-        for (int ks = r * 4; ks < KS && ks < r * 4 + 4; ++ks) {
-            i32x4 x = {0, 0, 0, 0};
-            uint32_t sc = 0;
-            if (live && ks < ksteps) {
-                x = *reinterpret_cast<const i32x4 *>(codes + row * (ksteps * 64) + ks * 64 + g * 16);
-                sc = scales[row * (ksteps * 4) + ks * 4 + g];
+            for (int b = 0; b < 4; ++b) {
+                const int ks = r * 4 + b;
+                if (ks >= KS) break;
+                i32x4 x = {0, 0, 0, 0};
+                uint32_t sc = 0;
+                if (live && ks < ksteps) {
+                    x = *reinterpret_cast<const i32x4 *>(codes + row * (ksteps * 64) + ks * 64 + g * 16);
+                    sc = scales[row * (ksteps * 4) + ks * 4 + g];
+                }
+                *reinterpret_cast<i32x4 *>(t + ks * 1024 + lane * 16) = x;
+                packed |= sc << (8 * b);
+                float e = 0.0f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float v[8];
+                    mx_decode8<4>(u32x2{(uint32_t)x[c], 0}, v);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) e = fmaf(v[u], v[u], e);
+                }
+                const double f = mx_factor(sc);
+                q += (double)e * f * f;
             }
-            *reinterpret_cast<i32x4 *>(t + ks * 1024 + lane * 16) = x;
-            packed |= sc << (8 * (ks % 4));
-            float e = 0.0f;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                float v[8];
-                mx_decode8<4>(u32x2{(uint32_t)x[c], 0}, v);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) e = fmaf(v[u], v[u], e);
-            }
-            const double f = mx_factor(sc);
-            q += (double)e * f * f;
+            if (r < (KS + 3) / 4) *reinterpret_cast<uint32_t *>(t + T::SCALES + r * 256 + lane * 4) = packed;
         }
-        *reinterpret_cast<uint32_t *>(t + T::SCALES + r * 256 + lane * 4) = packed;
     }
     q += __shfl_xor(q, 16);
     q += __shfl_xor(q, 32);
-    if (g == 0) *reinterpret_cast<float *>(t + T::BIAS + lr * 4) = live ? (float)(-0.5 * q) : -FLT_MAX;
+    if constexpr (WPT > 1) {
+        if (g == 0) part[wave][lr] = q;
+        __syncthreads();
+        q = 0.0;
+#pragma unroll
+        for (int w = 0; w < WPT; ++w) q += part[wave / WPT * WPT + w][lr];
+    }
+    if (there && turn == 0 && g == 0) *reinterpret_cast<float *>(t + T::BIAS + lr * 4) = live ? (float)(-0.5 * q) : -FLT_MAX;
 }
 
 // How a launch splits its work: set groups per workgroup, chosen by rounds of
@@ -280,8 +297,8 @@ template <int KS, int RT>
 hipError_t mx_sets_run(const MxSetsArgs &x, hipStream_t st) {
     const int64_t groups = x.lpad / 16, slots = (x.k + 1) / 2 * 2, ntiles = groups * slots;
     if (x.k > (1 << 24) || groups > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(mx_sets_pack_kernel<KS>, flat_grid((ntiles + 3) / 4, 256), dim3(256), 0, st, x.codes, x.scales, x.n,
-                       (int)(mx_padded(x.d) / kMxRow), x.sets, x.l, (int)x.k, ntiles, x.work);
+    hipLaunchKernelGGL(mx_sets_pack_kernel<KS>, flat_grid((ntiles * mx_pack_waves(KS) + 3) / 4, 256), dim3(256), 0, st, x.codes,
+                       x.scales, x.n, (int)(mx_padded(x.d) / kMxRow), x.sets, x.l, (int)x.k, ntiles, x.work);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     int64_t gpc = 1, gpc2 = 1;
