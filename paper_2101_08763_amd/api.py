@@ -422,9 +422,9 @@ def exemplar_rmsnorm(x, weight=None, residual=None, eps=1e-6, format=None, strea
     if residual is not None and (residual.dtype != dtype or residual.shape != x.shape):
         raise ValueError("residual must have x's type and shape")
     rstd = torch.empty(n, dtype=torch.float32, device=device)
-    h = x if residual is None else torch.empty((n, d), dtype=dtype, device=device)
+    h = x if residual is None else torch.empty_like(residual)
     if format is None or format == EXEMCL_MX_NONE:
-        y = codes = torch.empty((n, d), dtype=dtype, device=device)
+        y = codes = torch.empty_like(x)
         scales, format = None, EXEMCL_MX_NONE
     else:
         y = _mx_empty(n, d, format, device)
@@ -442,7 +442,7 @@ def exemplar_rmsnorm_backward(dy, h, weight, rstd, dh=None, stream=None):
     import torch
     if h.dim() != 2:
         raise ValueError("h must be n x d")
-    dtype, device = h.dtype, h.device
+    dtype = h.dtype
     prec = _precision(dtype)
     n, d = h.shape
     for t, name in ((dy, "dy"), (dh, "dh")):
@@ -452,8 +452,8 @@ def exemplar_rmsnorm_backward(dy, h, weight, rstd, dh=None, stream=None):
         raise ValueError("weight must have h's type and d elements")
     if rstd.dtype != torch.float32 or rstd.shape != (n,):
         raise ValueError("rstd must be float32 with n elements")
-    dx = torch.empty((n, d), dtype=dtype, device=device)
-    dw = torch.empty(d, dtype=torch.float32, device=device)
+    dx = torch.empty_like(h)
+    dw = torch.empty(d, dtype=torch.float32, device=h.device)
     _run("exemplar_rmsnorm_backward", (h, dy, weight, rstd, dh), stream, dy.data_ptr(), h.data_ptr(), _at(weight),
          rstd.data_ptr(), _at(dh), n, d, prec, dx.data_ptr(), dw.data_ptr())
     return dx, dw

@@ -5,12 +5,12 @@ namespace exemcl {
 
 hipError_t mx_sets_short(int ks, const MxSetsArgs &x, hipStream_t st) {
     switch (ks) {
-    case 1: return mx_sets_run<1, 8>(x, st);
-    case 2: return mx_sets_run<2, 8>(x, st);
-    case 3: return mx_sets_run<3, 6>(x, st);
-    case 4: return mx_sets_run<4, 6>(x, st);
-    case 5: return mx_sets_run<5, 4>(x, st);
-    default: return mx_sets_run<6, 4>(x, st);
+    case 1: return mx_sets_run<1, 8, 4>(x, st);
+    case 2: return mx_sets_run<2, 8, 4>(x, st);
+    case 3: return mx_sets_run<3, 8, 4>(x, st);
+    case 4: return mx_sets_run<4, 8, 4>(x, st);
+    case 5: return mx_sets_run<5, 4, 4>(x, st);
+    default: return mx_sets_run<6, 4, 4>(x, st);
     }
 }
 

@@ -10,6 +10,15 @@
 // the set group ends.  Rows past n read as zeros and add nothing, a bias being
 // at most 0.  A sum of every 32 points is written, in the same order whatever
 // RT and WAVES are, so these follow the launch and not the result.
+//
+// What bounds it is the matrix cores: 512 sets of 32 on 200 000 x 256 take 361 us
+// (4.6 PFLOP/s; the instruction alone, on random values, runs at 6.8), 512 of 16
+// on 20 000 x 1 536 131.  Two workgroups of 4 wavefronts to a CU beat one of 8,
+// which meets at a barrier every stage (396 us, and 261 against 209 at 128
+// coordinates); above 768 coordinates, where two row tiles are all that fit
+// beside 8 or more fragments each, LDS has room for one workgroup, and one of 8
+// wavefronts covers its LDS reads better (100 000 x 1 536, 256 of 16: 382 us, one
+// of 4 471; now 354 with more set groups to a workgroup).
 #pragma once
 
 #include <float.h>
@@ -254,18 +263,22 @@ __global__ __launch_bounds__(256) void mx_sets_pack_kernel(const uint8_t *__rest
 }
 
 // How a launch splits its work: set groups per workgroup, chosen by rounds of
-// workgroups over the CUs, times a group's instructions and what a workgroup
-// starts with (its points, the first stages: about 4 000 clocks).
+// workgroups over the CUs, times the instructions of the groups a CU works on
+// and what a workgroup starts with (the first stages and its points).  Two row
+// tiles leave LDS reads about as long as the instructions, and one wavefront to
+// a SIMD little to cover them.
 template <int KS, int RT, int WAVES>
 double mx_sets_cost(const MxSetsArgs &x, int64_t groups, int64_t *gpc) {
     using P = MxSetsPlan<KS, RT, WAVES>;
-    const int64_t nrb = (x.n + P::ROWS - 1) / P::ROWS;
-    const int64_t resident = std::max<int64_t>(1, device_cu_count()) * std::min(WAVES <= 4 ? 4 : 1, kLdsBytes / P::LDS);
-    const double group = (double)x.k * KS * RT * 16.0 * 2.0, start = 4000.0;
+    const int64_t nrb = (x.n + P::ROWS - 1) / P::ROWS, cus = std::max<int64_t>(1, device_cu_count());
+    const int64_t resident = std::min(WAVES > 4 ? 1 : RT > 2 ? 2 : 4, kLdsBytes / P::LDS);
+    const double stall = RT > 2 ? 1.0 : resident * WAVES > 4 ? 1.5 : 1.9;
+    const double group = (double)x.k * KS * RT * 16.0 * (WAVES / 4) * stall, start = 4000.0 + 500.0 * KS;
     double best = 0.0;
     for (int64_t c = 1; c <= groups; c = c < 16 ? c + 1 : c + c / 8) {
-        const int64_t wgs = nrb * ((groups + c - 1) / c), rounds = (wgs + resident - 1) / resident;
-        const double cost = (double)rounds * ((double)c * group + start);
+        const int64_t wgs = nrb * ((groups + c - 1) / c), each = std::min(resident, (wgs + cus - 1) / cus);
+        const int64_t rounds = (wgs + cus * resident - 1) / (cus * resident);
+        const double cost = (double)rounds * ((double)(c * each) * group + start);
         if (c == 1 || cost < best) best = cost, *gpc = c;
     }
     return best;
@@ -292,8 +305,8 @@ hipError_t mx_sets_launch(const MxSetsArgs &x, int64_t groups, int64_t gpc, hipS
 }
 
 // Tiles, then the sums: wavefronts with RT row tiles where the points fill the
-// chip that way, small workgroups of two where they do not.
-template <int KS, int RT>
+// chip that way, workgroups of four with two where they do not.
+template <int KS, int RT, int WAVES>
 hipError_t mx_sets_run(const MxSetsArgs &x, hipStream_t st) {
     const int64_t groups = x.lpad / 16, slots = (x.k + 1) / 2 * 2, ntiles = groups * slots;
     if (x.k > (1 << 24) || groups > INT32_MAX) return hipErrorInvalidValue;
@@ -302,9 +315,8 @@ hipError_t mx_sets_run(const MxSetsArgs &x, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     int64_t gpc = 1, gpc2 = 1;
-    // (two row tiles per fragment: LDS reads bound it, twice the time)
-    if (mx_sets_cost<KS, RT, 8>(x, groups, &gpc) <= 2.0 * mx_sets_cost<KS, 2, 4>(x, groups, &gpc2))
-        return mx_sets_launch<KS, RT, 8>(x, groups, gpc, st);
+    if (mx_sets_cost<KS, RT, WAVES>(x, groups, &gpc) <= mx_sets_cost<KS, 2, 4>(x, groups, &gpc2))
+        return mx_sets_launch<KS, RT, WAVES>(x, groups, gpc, st);
     return mx_sets_launch<KS, 2, 4>(x, groups, gpc2, st);
 }
 
