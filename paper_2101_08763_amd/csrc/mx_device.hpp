@@ -138,13 +138,17 @@ __device__ __forceinline__ void load8(const T *p, int have, float (&v)[8]) {
     for (int i = 0; i < 8; ++i) v[i] = to_f32((T)x[i]);
 }
 
-template <typename T>
+// STREAM: past the caches, which the array does not fit.
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ void store8(T *p, int have, const float (&v)[8]) {
     if (have >= 8) {
         typename Chunk<T>::vec x;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = (T)v[i];
-        *reinterpret_cast<typename Chunk<T>::vec *>(p) = x;
+        if constexpr (STREAM)
+            __builtin_nontemporal_store(x, reinterpret_cast<typename Chunk<T>::vec *>(p));
+        else
+            *reinterpret_cast<typename Chunk<T>::vec *>(p) = x;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
