@@ -300,7 +300,9 @@ EXEMCL_API int exemplar_sqnorm(const void *V, int64_t n, int64_t d, int precisio
  * streams, asynchrony) hold for these calls too, but n may be 0 (nothing is
  * queued then, and the arrays may be NULL), and infinities and NaN are defined
  * where a call says so.  Outputs must not overlap inputs unless a call says
- * that they may.
+ * that they may.  exemplar_rmsnorm_backward with dweight and exemplar_mx_eval
+ * take temporary memory as exemplar_eval does, so they are not for code under
+ * HIP graph capture; the others take none and may be captured.
  * ------------------------------------------------------------------------ */
 enum exemcl_mx_format {
     EXEMCL_MX_NONE = 0, /* exemplar_rmsnorm only: rows of the input's type */

@@ -36,6 +36,7 @@ namespace exemcl {
 
 constexpr int kMxSetRows = 32;        // points per partial sum
 constexpr int64_t kMxSetsD = 2048;    // longest rows kept in registers
+constexpr int64_t kMxGatherUnits = 8; // pairs of members a workgroup stages itself
 
 // Arguments of one launch: tiles (or biases) go to `work`.
 struct MxSetsArgs {
@@ -75,10 +76,90 @@ struct MxSetsPlan {
     static_assert(LDS <= kLdsBytes && RT % 2 == 0, "geometry");
 };
 
-template <int KS, int RT, int WAVES>
+// One tile, member p of the 16 sets of group grp, by WPT wavefronts of a
+// workgroup that take turns of four fragments (WPT = 1: any one wavefront).
+// |s|^2 in 64 bits (the squares of a block's elements add up to a whole number
+// of quarters); `part`: LDS, 16 doubles a wavefront.  `there` false: nothing is
+// read or written.
+template <int KS, int WPT>
+__device__ __forceinline__ void mx_pack_tile(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t n,
+                                             int ksteps, const int32_t *__restrict__ sets, int64_t l, int k, int64_t grp,
+                                             int p, bool there, uint8_t *t, double (*part)[16]) {
+    using T = MxTile<KS>;
+    const int wave = threadIdx.x >> 6, turn = wave % WPT, lane = threadIdx.x & 63, lr = lane & 15, g = lane >> 4;
+    const int64_t j = grp * 16 + lr;
+    const int64_t s = there ? sets[min(j, l - 1) * k + p] : -1;
+    const bool live = there && j < l && s >= 0 && s < n;
+    const int64_t row = live ? s : 0;
+    double q = 0.0;
+    if (there) {
+#pragma unroll
+        for (int r0 = 0; r0 < (KS + 3) / 4; r0 += WPT) {
+            const int r = r0 + turn;
+            uint32_t packed = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int ks = r * 4 + b;
+                if (ks >= KS) break;
+                i32x4 x = {0, 0, 0, 0};
+                uint32_t sc = 0;
+                if (live && ks < ksteps) {
+                    x = *reinterpret_cast<const i32x4 *>(codes + row * (ksteps * 64) + ks * 64 + g * 16);
+                    sc = scales[row * (ksteps * 4) + ks * 4 + g];
+                }
+                *reinterpret_cast<i32x4 *>(t + ks * 1024 + lane * 16) = x;
+                packed |= sc << (8 * b);
+                float e = 0.0f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float v[8];
+                    mx_decode8<4>(u32x2{(uint32_t)x[c], 0}, v);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) e = fmaf(v[u], v[u], e);
+                }
+                const double f = mx_factor(sc);
+                q += (double)e * f * f;
+            }
+            if (r < (KS + 3) / 4) *reinterpret_cast<uint32_t *>(t + T::SCALES + r * 256 + lane * 4) = packed;
+        }
+    }
+    q += __shfl_xor(q, 16);
+    q += __shfl_xor(q, 32);
+    if constexpr (WPT > 1) {
+        if (g == 0) part[wave][lr] = q;
+        __syncthreads();
+        q = 0.0;
+#pragma unroll
+        for (int w = 0; w < WPT; ++w) q += part[wave / WPT * WPT + w][lr];
+    }
+    if (there && turn == 0 && g == 0) *reinterpret_cast<float *>(t + T::BIAS + lr * 4) = live ? (float)(-0.5 * q) : -FLT_MAX;
+}
+
+// Tiles (group, member) in memory; slots behind the last member are left alone.
+constexpr int mx_pack_waves(int ks) { return ks <= 4 ? 1 : ks <= 8 ? 2 : 4; }
+
+template <int KS>
+__global__ __launch_bounds__(256) void mx_sets_pack_kernel(const uint8_t *__restrict__ codes,
+                                                           const uint8_t *__restrict__ scales, int64_t n, int ksteps,
+                                                           const int32_t *__restrict__ sets, int64_t l, int k,
+                                                           int64_t ntiles, uint8_t *__restrict__ tiles) {
+    constexpr int WPT = mx_pack_waves(KS), TILES = 4 / WPT;
+    __shared__ double part[4][16];
+    const int64_t i = flat_block() * TILES + (threadIdx.x >> 6) / WPT;
+    const int slots = (k + 1) / 2 * 2;
+    const int64_t grp = i / slots;
+    const int p = (int)(i - grp * slots);
+    mx_pack_tile<KS, WPT>(codes, scales, n, ksteps, sets, l, k, grp, p, i < ntiles && p < k,
+                          tiles + i * MxTile<KS>::BYTES, part);
+}
+
+// GATHER: the workgroup makes its tiles itself, all of them at once in LDS (they
+// fit), from the sets.
+template <int KS, int RT, int WAVES, bool GATHER>
 __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *__restrict__ codes,
                                                                 const uint8_t *__restrict__ scales, int64_t n, int ksteps,
-                                                                const uint8_t *__restrict__ tiles, int members,
+                                                                const uint8_t *__restrict__ tiles,
+                                                                const int32_t *__restrict__ sets, int64_t l, int members,
                                                                 int ngroups, int gpc, int nrb,
                                                                 float *__restrict__ partials, int64_t lpad) {
     using P = MxSetsPlan<KS, RT, WAVES>;
@@ -95,7 +176,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
     const int groups = (int)min((int64_t)gpc, ngroups - g0), pairs = (members + 1) / 2, units = groups * pairs;
 
     const uint8_t *stream = tiles + g0 * pairs * (int64_t)P::UNIT;
-    const int stages = (units + P::UPS - 1) / P::UPS;
+    const int stages = GATHER ? 1 : (units + P::UPS - 1) / P::UPS, ups = GATHER ? units : P::UPS;
     auto issue = [&](int st) {
         const int64_t at = (int64_t)st * P::STAGE, left = (int64_t)units * P::UNIT - at;
         const auto win = window_rsrc(stream + at, (uint32_t)max((int64_t)0, min((int64_t)P::STAGE, left)));
@@ -104,8 +185,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
         for (int i = 0; i < P::LOADS; ++i)
             window_to_lds16(win, buf + (i * P::THREADS + wave * 64) * 16, (uint32_t)((i * P::THREADS + tid) * 16));
     };
-    issue(0);
-    issue(1);
+    if constexpr (GATHER) {
+        for (int i = wave; i < 2 * units; i += WAVES) {
+            const int q = i / (2 * pairs), p = i - q * 2 * pairs;
+            mx_pack_tile<KS, 1>(codes, scales, n, ksteps, sets, l, members, g0 + q, p, p < members, smem + i * T::BYTES, nullptr);
+        }
+    } else {
+        issue(0);
+        issue(1);
+    }
 
     // The points, and their scales as the tiles have theirs.
     const int row_bytes = ksteps * 64, row_scales = ksteps * 4;
@@ -153,11 +241,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
     int q = 0;
     int64_t grp = g0;
     for (int st = 0; st < stages; ++st) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P::LOADS) : "memory");
+        if constexpr (!GATHER) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P::LOADS) : "memory");
         __syncthreads();
-        issue(st + 2);
+        if constexpr (!GATHER) issue(st + 2);
         const unsigned char *buf = smem + st % 3 * P::BUF;
-        const int last = min(P::UPS, units - st * P::UPS);
+        const int last = min(ups, units - st * ups);
         for (int u = 0; u < last; ++u) {
             const unsigned char *t = buf + u * P::UNIT;
             f32x4 x[RT], y[RT];
@@ -193,75 +281,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
 }
 
-// Tile (group, member) of l sets of k members, WPT wavefronts each, which take
-// turns of four fragments; |s|^2 in 64 bits (the squares of a block's elements
-// add up to a whole number of quarters).  Slots behind the last member are left
-// alone.
-constexpr int mx_pack_waves(int ks) { return ks <= 4 ? 1 : ks <= 8 ? 2 : 4; }
-
-template <int KS>
-__global__ __launch_bounds__(256) void mx_sets_pack_kernel(const uint8_t *__restrict__ codes,
-                                                           const uint8_t *__restrict__ scales, int64_t n, int ksteps,
-                                                           const int32_t *__restrict__ sets, int64_t l, int k,
-                                                           int64_t ntiles, uint8_t *__restrict__ tiles) {
-    using T = MxTile<KS>;
-    constexpr int WPT = mx_pack_waves(KS), TILES = 4 / WPT;
-    __shared__ double part[4][16];
-    const int wave = threadIdx.x >> 6, turn = wave % WPT;
-    const int64_t i = flat_block() * TILES + wave / WPT;
-    const int lane = threadIdx.x & 63, lr = lane & 15, g = lane >> 4;
-    const int slots = (k + 1) / 2 * 2;
-    const int64_t grp = i / slots, j = grp * 16 + lr;
-    const int p = (int)(i - grp * slots);
-    const bool there = i < ntiles && p < k;
-    const int64_t s = there ? sets[min(j, l - 1) * k + p] : -1;
-    const bool live = there && j < l && s >= 0 && s < n;
-    const int64_t row = live ? s : 0;
-    uint8_t *t = tiles + i * T::BYTES;
-    double q = 0.0;
-    if (there) {
-#pragma unroll
-        for (int r0 = 0; r0 < (KS + 3) / 4; r0 += WPT) {
-            const int r = r0 + turn;
-            uint32_t packed = 0;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int ks = r * 4 + b;
-                if (ks >= KS) break;
-                i32x4 x = {0, 0, 0, 0};
-                uint32_t sc = 0;
-                if (live && ks < ksteps) {
-                    x = *reinterpret_cast<const i32x4 *>(codes + row * (ksteps * 64) + ks * 64 + g * 16);
-                    sc = scales[row * (ksteps * 4) + ks * 4 + g];
-                }
-                *reinterpret_cast<i32x4 *>(t + ks * 1024 + lane * 16) = x;
-                packed |= sc << (8 * b);
-                float e = 0.0f;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    float v[8];
-                    mx_decode8<4>(u32x2{(uint32_t)x[c], 0}, v);
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) e = fmaf(v[u], v[u], e);
-                }
-                const double f = mx_factor(sc);
-                q += (double)e * f * f;
-            }
-            if (r < (KS + 3) / 4) *reinterpret_cast<uint32_t *>(t + T::SCALES + r * 256 + lane * 4) = packed;
-        }
-    }
-    q += __shfl_xor(q, 16);
-    q += __shfl_xor(q, 32);
-    if constexpr (WPT > 1) {
-        if (g == 0) part[wave][lr] = q;
-        __syncthreads();
-        q = 0.0;
-#pragma unroll
-        for (int w = 0; w < WPT; ++w) q += part[wave / WPT * WPT + w][lr];
-    }
-    if (there && turn == 0 && g == 0) *reinterpret_cast<float *>(t + T::BIAS + lr * 4) = live ? (float)(-0.5 * q) : -FLT_MAX;
-}
-
 // How a launch splits its work: set groups per workgroup, chosen by rounds of
 // workgroups over the CUs, times the instructions of the groups a CU works on
 // and what a workgroup starts with (the first stages and its points).  Two row
@@ -284,10 +303,10 @@ double mx_sets_cost(const MxSetsArgs &x, int64_t groups, int64_t *gpc) {
     return best;
 }
 
-template <int KS, int RT, int WAVES>
+template <int KS, int RT, int WAVES, bool GATHER = false>
 hipError_t mx_sets_launch(const MxSetsArgs &x, int64_t groups, int64_t gpc, hipStream_t st) {
     using P = MxSetsPlan<KS, RT, WAVES>;
-    auto kern = mx_sets_kernel<KS, RT, WAVES>;
+    auto kern = mx_sets_kernel<KS, RT, WAVES, GATHER>;
     static std::atomic<bool> ready[kMaxDevices];  // the attribute holds for one device
     const int dev = current_device();
     if (dev < 0) return hipErrorInvalidDevice;
@@ -299,8 +318,8 @@ hipError_t mx_sets_launch(const MxSetsArgs &x, int64_t groups, int64_t gpc, hipS
     const int64_t nrb = (x.n + P::ROWS - 1) / P::ROWS;
     if (gpc * ((x.k + 1) / 2) > (1 << 30)) return hipErrorInvalidValue;
     hipLaunchKernelGGL(kern, flat_grid(nrb * ((groups + gpc - 1) / gpc), P::THREADS), dim3(P::THREADS), P::LDS, st, x.codes,
-                       x.scales, x.n, (int)(mx_padded(x.d) / kMxRow), x.work, (int)x.k, (int)groups, (int)gpc, (int)nrb,
-                       x.partials, x.lpad);
+                       x.scales, x.n, (int)(mx_padded(x.d) / kMxRow), x.work, x.sets, x.l, (int)x.k, (int)groups, (int)gpc,
+                       (int)nrb, x.partials, x.lpad);
     return hipGetLastError();
 }
 
@@ -310,13 +329,21 @@ template <int KS, int RT, int WAVES>
 hipError_t mx_sets_run(const MxSetsArgs &x, hipStream_t st) {
     const int64_t groups = x.lpad / 16, slots = (x.k + 1) / 2 * 2, ntiles = groups * slots;
     if (x.k > (1 << 24) || groups > INT32_MAX) return hipErrorInvalidValue;
+    int64_t gpc = 1, gpc2 = 1;
+    const bool large = mx_sets_cost<KS, RT, WAVES>(x, groups, &gpc) <= mx_sets_cost<KS, 2, 4>(x, groups, &gpc2);
+    // Few short tiles: each workgroup makes its own, which saves the launch that
+    // stages them (10 000 x 64, 48 sets of 8: 13.3 -> 10.2 us a call).
+    if constexpr (KS <= 2) {
+        using P = MxSetsPlan<KS, 2, 4>;
+        const int64_t units = gpc2 * slots / 2;
+        if (!large && units <= kMxGatherUnits && units * P::UNIT <= P::LDS)
+            return mx_sets_launch<KS, 2, 4, true>(x, groups, gpc2, st);
+    }
     hipLaunchKernelGGL(mx_sets_pack_kernel<KS>, flat_grid((ntiles * mx_pack_waves(KS) + 3) / 4, 256), dim3(256), 0, st, x.codes,
                        x.scales, x.n, (int)(mx_padded(x.d) / kMxRow), x.sets, x.l, (int)x.k, ntiles, x.work);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    int64_t gpc = 1, gpc2 = 1;
-    if (mx_sets_cost<KS, RT, WAVES>(x, groups, &gpc) <= mx_sets_cost<KS, 2, 4>(x, groups, &gpc2))
-        return mx_sets_launch<KS, RT, WAVES>(x, groups, gpc, st);
+    if (large) return mx_sets_launch<KS, RT, WAVES>(x, groups, gpc, st);
     return mx_sets_launch<KS, 2, 4>(x, groups, gpc2, st);
 }
 

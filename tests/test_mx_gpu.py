@@ -413,6 +413,65 @@ def test_sets_many():
     assert np.all(np.abs(got[at] - want) <= 1e-5 * np.abs(want) + 1e-7 * (V * V).sum(1).mean())
 
 
+# -- past 32 bits -----------------------------------------------------------------
+def test_rows_past_32_bits():
+    """Inputs, codes and results whose last elements lie past 2^31 elements and
+    2^32 bytes, checked at both ends."""
+    n, d = 1_450_000, 1536
+    x = torch.empty(n, d, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    ends = [0, 1, n // 2, n - 2, n - 1]
+    for fmt in (FP4, FP8):
+        q = api.exemplar_mx_quantize(x, fmt)
+        want = ref.quantize(to64(x[ends]), fmt)
+        codes, scales = q.codes[ends].cpu().numpy(), q.scales[ends].cpu().numpy()
+        assert np.array_equal(scales, want[1])
+        assert np.array_equal(ref.values(codes, scales, d, fmt), ref.values(*want, d, fmt))
+        back = api.exemplar_mx_dequantize(q, torch.bfloat16)
+        assert np.array_equal(to64(back[ends]), ref.values(codes, scales, d, fmt))
+        del back
+    y, _, rstd = api.exemplar_rmsnorm(x, eps=0.0)
+    want, _, s = ref.rmsnorm(to64(x[ends]), None, None, 0.0)
+    assert np.all(np.abs(to64(rstd[ends]) - s) <= 2.5e-6 * s)
+    assert np.all(np.abs(to64(y[ends]) - want) <= (2.5e-6 + UNIT[torch.bfloat16] * 1.001) * np.abs(want))
+    dx, _ = api.exemplar_rmsnorm_backward(x, y, None, rstd)
+    want, _ = ref.rmsnorm_backward(to64(x[ends]), to64(y[ends]), None, to64(rstd[ends]), None)
+    assert np.all(np.abs(to64(dx[ends]) - want) <= 2.5e-6 * 60 + UNIT[torch.bfloat16] * 1.001 * np.abs(want))
+
+
+def test_product_past_32_bits():
+    g = gen("wide product")
+    A, a = random_rows(g, 70_001, 40, FP8)
+    B, b = random_rows(g, 31_003, 40, FP4)
+    C = api.exemplar_mx_product(A, B, dtype=torch.float16)
+    rows, cols = [0, 35_000, 69_272, 70_000], [0, 1, 15_000, 31_002]
+    want, size = a[rows] @ b[cols].T, np.abs(a[rows]) @ np.abs(b[cols]).T
+    got = to64(C[rows][:, cols])
+    assert np.all(np.abs(got - want) <= 2.0 ** -10 * size + UNIT[torch.float16] * 1.01 * np.abs(want) + TINY[torch.float16])
+
+
+def test_sets_past_32_bits():
+    """4-bit rows of 4.6 GB; scores against the products' own values in 64 bits,
+    a block of points at a time."""
+    n, d = 6_000_000, 1500
+    g = torch.Generator("cuda").manual_seed(3)
+    q = api.MxRows(torch.randint(0, 256, (n, 768), dtype=torch.uint8, device="cuda", generator=g),
+                   torch.randint(120, 124, (n, 48), dtype=torch.uint8, device="cuda", generator=g), d, FP4)
+    q.codes[:, 750:] = 0
+    sets = torch.tensor([[0, n - 1, n // 2], [5_999_990, -1, 5_700_000], [7, 8, n]], dtype=torch.int32)
+    got = to64(api.exemplar_mx_eval(q, sets.cuda()))
+    assert np.isnan(got[2])
+    member = [i for i in sets[:2].flatten().tolist() if i >= 0]
+    E = torch.as_tensor(ref.values(q.codes[member].cpu().numpy(), q.scales[member].cpu().numpy(), d, FP4), device="cuda")
+    total, norms = torch.zeros(2, dtype=torch.float64, device="cuda"), 0.0
+    for i in range(0, n, 500_000):
+        V = api.exemplar_mx_dequantize(api.MxRows(q.codes[i:i + 500_000], q.scales[i:i + 500_000], d, FP4), torch.float32).double()
+        h = V @ E.t().contiguous() - 0.5 * (E * E).sum(1)
+        total += torch.stack((h[:, :3].amax(1).clamp(min=0).sum(), h[:, 3:].amax(1).clamp(min=0).sum()))
+        norms += float((V * V).sum())
+    want = to64(total) * 2 / n
+    assert np.all(np.abs(got[:2] - want) <= 1e-5 * np.abs(want) + 1e-7 * norms / n)
+
+
 # -- together -----------------------------------------------------------------------
 def test_norm_product_and_sets_together():
     """Hidden states to scores: norm to 8 bits, projection by 4-bit weights,
