@@ -74,11 +74,11 @@ __global__ __launch_bounds__(kDirectWaves * 64) void mx_product_direct_kernel(
 // own order, takes the address units 64 steps a load instead of 16: 16 384 x
 // 8 192 x 4 096 565 us).
 //
-// That size, 8 by 4 bits to bf16, takes 404 us (2.7 PFLOP/s; the instruction
-// alone, on random values, runs at 4.2), 256 x 256 x 128 in 1.24 us a stage of
-// which 0.85 are instructions.  With zeros for data it is 388: on others the
-// chip lowers its clock.  What is left is the start and the end of a tile (71 us
-// in all, 256 x 256), LDS reads and copies between instructions.
+// That size, 8 by 4 bits to bf16, takes 416 us (2.65 PFLOP/s; the instruction
+// alone, on random values, runs at 4.2), 4 by 4 bits 303 (3.6 of 6.8).  With zeros
+// for data it is 385: on others the chip lowers its clock.  The rest is the start
+// and the end of a tile, LDS reads and copies between instructions: wavefronts of
+// 128 x 128, 128 x 64 or 64 x 128 end within 3 % of each other.
 // ---------------------------------------------------------------------------
 template <int BITS_A, int WM, int NB, int PM, int PN, int DEPTH>
 struct MxTilePlan {
@@ -100,12 +100,12 @@ struct MxTilePlan {
     static constexpr int B_AT = A_FRAGS * 1024, BUF = B_AT + B_FRAGS * 1024;
     static constexpr int SCALES_AT = DEPTH * BUF, SBUF = S_LOADS * THREADS * 16, LDS = SCALES_AT + 2 * SBUF;
     static_assert(A_FRAGS % WAVES == 0 && B_FRAGS % WAVES == 0 && BM % 64 == 0 &&
-                      4 * NB % WM == 0 && LDS <= kLdsBytes,
+                      LDS <= kLdsBytes,
                   "geometry");
 };
 
 template <typename T, int BITS_A, bool DIVIDE, int WM, int NB, int PM, int PN, int DEPTH>
-__global__ __launch_bounds__(PM *PN * 64, WM * NB > 8 ? 1 : 2) void mx_product_kernel(
+__global__ __launch_bounds__(PM *PN * 64, 2) void mx_product_kernel(
     const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, int64_t m, const uint8_t *__restrict__ B,
     const uint8_t *__restrict__ Bs, int64_t n, int ksteps, int mblocks, int nblocks, const float *__restrict__ bias,
     T *__restrict__ C) {
@@ -426,10 +426,12 @@ hipError_t product_tiled(const MxProductArgs &a, hipStream_t st) {
 //   130 x 8 192 x 1 024     25.1    10.3     11.0     14.9     20.5
 //   1 024 x 8 192 x 1 024            22.6     16.9     18.7     23.8
 //   1 024 x 30 000 x 1 024           64.4     47.8     42.8     48.2
-//   16 384 x 8 192 x 1 024                   157      128      155
-//   16 384 x 8 192 x 4 096                   491      426      404
-// The largest has one workgroup per CU and starts and ends alone: it wins from
-// about 3 000 coordinates on, where its last round is full.
+//   16 384 x 8 192 x 1 024                   157      130      153
+//   16 384 x 8 192 x 4 096                   491      424      416
+// The largest has one workgroup per CU, which starts and ends alone: it wins
+// from about 3 000 coordinates on (1 500 with 4-bit rows), where its last round is
+// full.  Rows in two parts take 128 x 256: two workgroups per CU cover the
+// division (16 384 x 8 192 x 4 096 to fp32: 711 us, the largest 890).
 template <typename T, int BITS_A, bool DIVIDE>
 hipError_t product_run(const MxProductArgs &a, hipStream_t st) {
     const int64_t cus = std::max<int64_t>(1, device_cu_count());
@@ -442,7 +444,9 @@ hipError_t product_run(const MxProductArgs &a, hipStream_t st) {
     if (tiles(64, 128) <= cus) return product_tiled<T, BITS_A, DIVIDE, 4, 1, 1, 2, 3>(a, st);
     if (tiles(128, 128) <= 3 * cus) return product_tiled<T, BITS_A, DIVIDE, 4, 1, 2, 2, 3>(a, st);
     const int64_t large = tiles(256, 256), last = (large + cus - 1) / cus * cus;
-    if (!DIVIDE && ks >= 24 && last * 10 <= large * 11) return product_tiled<T, BITS_A, DIVIDE, 8, 2, 2, 2, 3>(a, st);
+    if constexpr (!DIVIDE)
+        if (ks >= (BITS_A == 8 ? 24 : 12) && last * 10 <= large * 11)
+            return product_tiled<T, BITS_A, DIVIDE, 8, 1, 2, 4, 3>(a, st);
     return product_tiled<T, BITS_A, DIVIDE, 4, 2, 2, 2, 2>(a, st);
 }
 
