@@ -71,32 +71,45 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t *__res
 // the row stays in registers (CPT chunks a thread) between the sum of squares
 // and the result.  CPT = 0: rows too long for that, read twice.  HBM-bound:
 // 20 000 x 1 536 bf16 with a residual to 8 bits in 37 us (5.9 TB/s).
+//
+// The sum and its root are held in 64 bits, and v times the root's two 32-bit
+// parts is rounded once before w's product: a row's last bit decides on which
+// side of a power of two a block's maximum falls, and with it the whole block's
+// scale.  It takes no time: the kernel waits for memory.
 // ---------------------------------------------------------------------------
-template <int TPR>
-__device__ __forceinline__ float row_sum(float s, float *lds) {
+template <int TPR, typename S>
+__device__ __forceinline__ S row_sum(S s, S *lds) {
 #pragma unroll
     for (int off = min(TPR, 64) / 2; off >= 1; off >>= 1) s += __shfl_xor(s, off);
     if constexpr (TPR > 64) {
         __syncthreads();  // the last row's sums have been read
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
         __syncthreads();
-        s = 0.0f;
+        s = 0;
 #pragma unroll
         for (int w = 0; w < TPR / 64; ++w) s += lds[w];
     }
     return s;
 }
 
+// 1 / sqrt(m): the instruction's 26 bits and one step of Newton's iteration.  Its
+// ends (m = 0, infinite, NaN) are the instruction's own.
+__device__ __forceinline__ double inverse_root(double m) {
+    const double r = __builtin_amdgcn_rsq(m), half = 0.5 * r;
+    const double t = fma(fma(-m * r, r, 1.0), half, r);
+    return r > 0.0 && r < (double)INFINITY ? t : r;
+}
+
 constexpr int norm_block(int tpr) { return tpr > 256 ? tpr : 256; }
 
 template <typename T, int BITS, int TPR, int CPT>
 __global__ __launch_bounds__(norm_block(TPR)) void rmsnorm_kernel(const T *x, const T *r,
-                                                                  const T *__restrict__ w, int64_t n, int d, float eps,
-                                                                  T *h, T *__restrict__ y, uint8_t *__restrict__ codes,
+                                                                  const T *__restrict__ w, int64_t n, int d,
+                                                                  double inv_d, float eps, T *h, T *__restrict__ y, uint8_t *__restrict__ codes,
                                                                   uint8_t *__restrict__ scales,
                                                                   float *__restrict__ rstd_out) {
     constexpr int RPB = norm_block(TPR) / TPR;
-    __shared__ float lds[TPR / 64 + 1];
+    __shared__ double lds[TPR / 64 + 1];
     const int t = threadIdx.x % TPR;
     const int64_t row = flat_block() * RPB + threadIdx.x / TPR;
     const bool live = row < n;
@@ -112,7 +125,7 @@ __global__ __launch_bounds__(norm_block(TPR)) void rmsnorm_kernel(const T *x, co
             for (int e = 0; e < 8; ++e) v[e] += u[e];
         }
     };
-    auto finish = [&](int c, const float(&v)[8], float rstd) {
+    auto finish = [&](int c, const float(&v)[8], float rstd, float low) {
         const int d0 = c * 8;
         if (h && live) store8(h + at + d0, d - d0, v);
         float g[8];
@@ -122,42 +135,46 @@ __global__ __launch_bounds__(norm_block(TPR)) void rmsnorm_kernel(const T *x, co
 #pragma unroll
             for (int e = 0; e < 8; ++e) g[e] = 1.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] *= v[e] * rstd;
+        for (int e = 0; e < 8; ++e) {
+            const float p = v[e] * rstd, rest = fmaf(v[e], low, fmaf(v[e], rstd, -p));
+            g[e] = fmaf(p, g[e], rest * g[e]);
+        }
         if constexpr (BITS != 0)
             mx_store8<BITS>(g, live && c < chunks, codes + row * mx_row_bytes(d, BITS), scales + row * mx_row_scales(d), c);
         else if (live)
             store8(y + at + d0, d - d0, g);
     };
-    float s = 0.0f, rstd;
+    double s = 0.0;
     if constexpr (CPT > 0) {
         float v[CPT][8];
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
             load(t + i * TPR, v[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s = fmaf(v[i][e], v[i][e], s);
+            for (int e = 0; e < 8; ++e) s = fma((double)v[i][e], (double)v[i][e], s);
         }
-        rstd = 1.0f / sqrtf(row_sum<TPR>(s, lds) / (float)d + eps);
+        s = inverse_root(row_sum<TPR>(s, lds) * inv_d + (double)eps);
+        const float rstd = (float)s, low = (float)(s - rstd);
 #pragma unroll
-        for (int i = 0; i < CPT; ++i) finish(t + i * TPR, v[i], rstd);
+        for (int i = 0; i < CPT; ++i) finish(t + i * TPR, v[i], rstd, low);
     } else {
         for (int c = t; c < chunks; c += TPR) {
-            float v[8], q = 0.0f;
+            float v[8];
             load(c, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q = fmaf(v[e], v[e], q);
-            s += q;
+            for (int e = 0; e < 8; ++e) s = fma((double)v[e], (double)v[e], s);
         }
-        rstd = 1.0f / sqrtf(row_sum<TPR>(s, lds) / (float)d + eps);
+        s = inverse_root(row_sum<TPR>(s, lds) * inv_d + (double)eps);
+        const float rstd = (float)s, low = (float)(s - rstd);
         // whole blocks of four lanes take every step together (chunks is a
         // multiple of 4 where it matters)
         for (int c = t; c < chunks; c += TPR) {
             float v[8];
             load(c, v);
-            finish(c, v, rstd);
+            finish(c, v, rstd, low);
         }
     }
-    if (rstd_out && live && t == 0) rstd_out[row] = rstd;
+    if (rstd_out && live && t == 0) rstd_out[row] = (float)s;
 }
 
 // ---------------------------------------------------------------------------
@@ -363,8 +380,8 @@ template <typename T, int BITS, int TPR, int CPT>
 hipError_t norm_launch(const NormArgs &a, hipStream_t st) {
     constexpr int block = norm_block(TPR), rpb = block / TPR;
     hipLaunchKernelGGL((rmsnorm_kernel<T, BITS, TPR, CPT>), flat_grid((a.n + rpb - 1) / rpb, block), dim3(block), 0, st,
-                       (const T *)a.x, (const T *)a.residual, (const T *)a.weight, a.n, (int)a.d, a.eps, (T *)a.h,
-                       (T *)a.y, (uint8_t *)a.y, (uint8_t *)a.scales, a.rstd);
+                       (const T *)a.x, (const T *)a.residual, (const T *)a.weight, a.n, (int)a.d, 1.0 / a.d, a.eps,
+                       (T *)a.h, (T *)a.y, (uint8_t *)a.y, (uint8_t *)a.scales, a.rstd);
     return hipGetLastError();
 }
 
