@@ -855,23 +855,26 @@ int run_mx_eval(const void *codes, const void *scales, int64_t n, int64_t d, con
                 float *out, hipStream_t st) {
     if (l == 0) return EXEMCL_OK;
     if (k == 0) return status_of(launch_zero(out, l, st));
-    const int64_t G = mx_sets_parts(n), unit = kMxSets, limit = workspace_limit();
+    const int64_t G = mx_sets_parts(n), folds = mx_sets_folds(G), unit = kMxSets, limit = workspace_limit();
     int64_t lc = l, lpad = 0, off = 0;
     Scratch ws;
     for (;;) {
         lpad = align_up(lc, unit);
         off = align_up(lpad / unit * mx_sets_work(d, k), 256);
-        const int64_t bytes = off + G * lpad * 4;
+        const int64_t bytes = off + (G + folds) * lpad * 4;
         const int rc = bytes <= limit ? alloc_scratch(&ws, bytes, st) : EXEMCL_ENOMEM;
         if (rc == EXEMCL_OK) break;
         if (rc != EXEMCL_ENOMEM || lc <= unit) return rc;
         lc = align_up((lc + 1) / 2, unit);
     }
-    float *partials = (float *)((char *)ws.ptr + off);
+    float *partials = (float *)((char *)ws.ptr + off), *folded = partials + G * lpad;
     for (int64_t j0 = 0; j0 < l; j0 += lc) {
         const int64_t lj = std::min(lc, l - j0);
         hipError_t e = launch_mx_sets(codes, scales, n, d, sets + j0 * k, lj, k, ws.ptr, partials, lpad, st);
-        if (e == hipSuccess) e = launch_reduce(partials, G, lpad, lj, n, sets + j0 * k, k, nullptr, 0, out + j0, st);
+        if (e == hipSuccess && folds) e = launch_mx_fold(partials, G, lpad, lj, folded, st);
+        if (e == hipSuccess)
+            e = launch_reduce(folds ? folded : partials, folds ? folds : G, lpad, lj, n, sets + j0 * k, k, nullptr, 0,
+                              out + j0, st);
         if (e != hipSuccess) return EXEMCL_EDEVICE;
     }
     return EXEMCL_OK;

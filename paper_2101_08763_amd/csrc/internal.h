@@ -275,4 +275,9 @@ int64_t mx_sets_work(int64_t d, int64_t k);
 hipError_t launch_mx_sets(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets, int64_t l,
                           int64_t k, void *work, float *partials, int64_t lpad, hipStream_t st);
 
+// G rows of partials folded into mx_sets_folds(G) rows at `folded`; 0: too few
+// for it to pay.
+int64_t mx_sets_folds(int64_t G);
+hipError_t launch_mx_fold(const float *partials, int64_t G, int64_t lpad, int64_t l, float *folded, hipStream_t st);
+
 }  // namespace exemcl

@@ -11,9 +11,9 @@
 // at most 0.  A sum of every 32 points is written, in the same order whatever
 // RT and WAVES are, so these follow the launch and not the result.
 //
-// What bounds it is the matrix cores: 512 sets of 32 on 200 000 x 256 take 361 us
-// (4.6 PFLOP/s; the instruction alone, on random values, runs at 6.8), 512 of 16
-// on 20 000 x 1 536 131.  Two workgroups of 4 wavefronts to a CU beat one of 8,
+// What bounds it is the matrix cores: 512 sets of 32 on 200 000 x 256 take 353 us
+// (4.75 PFLOP/s; the instruction alone, on random values, runs at 6.8), 512 of 16
+// on 20 000 x 1 536 129.  Two workgroups of 4 wavefronts to a CU beat one of 8,
 // which meets at a barrier every stage (396 us, and 261 against 209 at 128
 // coordinates); above 768 coordinates, where two row tiles are all that fit
 // beside 8 or more fragments each, LDS has room for one workgroup, and one of 8

@@ -397,6 +397,19 @@ def test_sets_do_not_depend_on_the_batch(n, d, monkeypatch):
         limit //= 2
 
 
+@pytest.mark.parametrize("n", [131_040, 131_041, 200_003])
+def test_sets_on_many_points(n, monkeypatch):
+    """Around and past the number of partial sums that are added in two steps."""
+    q, V, sets = set_inputs(n, 20, 37, 4)
+    s = torch.as_tensor(sets).cuda()
+    f = api.exemplar_mx_eval(q, s)
+    want = ref.f_of_sets(V, sets)
+    assert np.all(np.abs(to64(f) - want) <= 1e-5 * np.abs(want) + 1e-7 * (V * V).sum(1).mean())
+    assert torch.equal(api.exemplar_mx_eval(q, s[20:21].contiguous()), f[20:21])
+    monkeypatch.setenv("EXEMCL_WORKSPACE_LIMIT", str(3 * 16 * 4 * (n // 32 + n // 1024)))
+    assert torch.equal(api.exemplar_mx_eval(q, s), f)
+
+
 def test_sets_of_no_sets_and_no_members():
     q, _, _ = set_inputs(50, 40, 1, 1)
     assert api.exemplar_mx_eval(q, torch.empty(0, 3, dtype=torch.int32, device="cuda")).shape == (0,)
