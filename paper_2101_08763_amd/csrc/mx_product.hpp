@@ -432,6 +432,10 @@ hipError_t product_tiled(const MxProductArgs &a, hipStream_t st) {
 // from about 3 000 coordinates on (1 500 with 4-bit rows), where its last round is
 // full.  Rows in two parts take 128 x 256: two workgroups per CU cover the
 // division (16 384 x 8 192 x 4 096 to fp32: 711 us, the largest 890).
+// Stores of fp32 results overlap less of what follows them, and 128 x 256 pays
+// earlier (333 x 30 011 x 301, 2.75 tiles of 128 x 128 a CU: 21.4 us instead of
+// 23.5).  With 4-bit rows two stages are enough for 128 x 128 and let three
+// workgroups share a CU (the same to bf16: 12.4 us instead of 15.4).
 template <typename T, int BITS_A, bool DIVIDE>
 hipError_t product_run(const MxProductArgs &a, hipStream_t st) {
     const int64_t cus = std::max<int64_t>(1, device_cu_count());
@@ -442,7 +446,8 @@ hipError_t product_run(const MxProductArgs &a, hipStream_t st) {
     const double tiled = 5.4 + (DIVIDE ? 0.9 : BITS_A == 8 ? 0.38 : 0.3) * ks;
     if (direct <= tiled * std::max(1.0, (double)tiles(64, 128) / (2.0 * cus))) return product_direct<T, BITS_A, DIVIDE>(a, st);
     if (tiles(64, 128) <= cus) return product_tiled<T, BITS_A, DIVIDE, 4, 1, 1, 2, 3>(a, st);
-    if (tiles(128, 128) <= 3 * cus) return product_tiled<T, BITS_A, DIVIDE, 4, 1, 2, 2, 3>(a, st);
+    if (tiles(128, 128) * 2 <= (sizeof(T) == 4 ? 5 : 6) * cus)
+        return product_tiled<T, BITS_A, DIVIDE, 4, 1, 2, 2, BITS_A == 8 ? 3 : 2>(a, st);
     const int64_t large = tiles(256, 256), last = (large + cus - 1) / cus * cus;
     if constexpr (!DIVIDE)
         if (ks >= (BITS_A == 8 ? 24 : 12) && last * 10 <= large * 11)
