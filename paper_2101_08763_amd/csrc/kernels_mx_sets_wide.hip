@@ -5,7 +5,7 @@ namespace exemcl {
 
 hipError_t mx_sets_wide(int ks, const MxSetsArgs &x, hipStream_t st) {
     switch (ks) {
-    case 8: return mx_sets_run<8, 2, 8>(x, st);
+    case 8: return mx_sets_run<8, 4, 4>(x, st);
     case 10: return mx_sets_run<10, 2, 8>(x, st);
     case 12: return mx_sets_run<12, 2, 8>(x, st);
     case 14: return mx_sets_run<14, 2, 8>(x, st);

@@ -11,14 +11,15 @@
 // at most 0.  A sum of every 32 points is written, in the same order whatever
 // RT and WAVES are, so these follow the launch and not the result.
 //
-// What bounds it is the matrix cores: 512 sets of 32 on 200 000 x 256 take 353 us
-// (4.75 PFLOP/s; the instruction alone, on random values, runs at 6.8), 512 of 16
-// on 20 000 x 1 536 129.  Two workgroups of 4 wavefronts to a CU beat one of 8,
-// which meets at a barrier every stage (396 us, and 261 against 209 at 128
-// coordinates); above 768 coordinates, where two row tiles are all that fit
-// beside 8 or more fragments each, LDS has room for one workgroup, and one of 8
-// wavefronts covers its LDS reads better (100 000 x 1 536, 256 of 16: 382 us, one
-// of 4 471; now 354 with more set groups to a workgroup).
+// What bounds it is the matrix cores: 512 sets of 32 on 200 000 x 256 take 335 us
+// (5.0 PFLOP/s; the instruction alone, on random values, runs at 6.8), 512 of 16
+// on 20 000 x 1 536 119.  Two workgroups of 4 wavefronts to a CU beat one of 8,
+// which meets at a barrier every stage (200 000 x 256: 396 us when the smaller
+// ones took 361; 100 000 x 1 024, 512 of 16: 400 against 340); above 1 024
+// coordinates, where two row tiles are all that fit beside 10 or more fragments
+// each, LDS has room for one workgroup, and one of 8 wavefronts covers its LDS
+// reads better (100 000 x 1 536, 256 of 16: 329 us; one wavefront to a SIMD with
+// four row tiles 332, and 163 against 147 at 1 792).
 #pragma once
 
 #include <float.h>
@@ -71,7 +72,13 @@ struct MxSetsPlan {
     static constexpr int UPS = UNIT >= 16384 ? 1 : 16384 / UNIT;            // units per stage
     static constexpr int STAGE = UPS * UNIT;
     static constexpr int LOADS = (STAGE + THREADS * 16 - 1) / (THREADS * 16);  // per thread
-    static constexpr int BUF = LOADS * THREADS * 16, LDS = 3 * BUF;
+    // The operands of a tile are read while the one before it computes, each over
+    // the one just used: 100 000 x 1 536, 256 sets of 16 329 us instead of 354,
+    // 50 000 x 768, 512 of 16 142 (150), 200 000 x 256, 512 of 32 346 (360).  Not
+    // for one fragment a tile (3 % slower), nor for four with 8 row tiles, which
+    // leave no registers (184 us instead of 110).
+    static constexpr bool AHEAD = WAVES > 4 || (RT > 2 && KS != 1 && KS != 4);
+    static constexpr int DEPTH = AHEAD ? 4 : 3, BUF = LOADS * THREADS * 16, LDS = DEPTH * BUF;
     static constexpr int ROWS = WAVES * RT * 16;
     static_assert(LDS <= kLdsBytes && RT % 2 == 0, "geometry");
 };
@@ -156,7 +163,7 @@ __global__ __launch_bounds__(256) void mx_sets_pack_kernel(const uint8_t *__rest
 // GATHER: the workgroup makes its tiles itself, all of them at once in LDS (they
 // fit), from the sets.
 template <int KS, int RT, int WAVES, bool GATHER>
-__global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *__restrict__ codes,
+__global__ __launch_bounds__(WAVES * 64, RT > 2 && WAVES == 4 && KS > 8 ? 1 : 2) void mx_sets_kernel(const uint8_t *__restrict__ codes,
                                                                 const uint8_t *__restrict__ scales, int64_t n, int ksteps,
                                                                 const uint8_t *__restrict__ tiles,
                                                                 const int32_t *__restrict__ sets, int64_t l, int members,
@@ -180,7 +187,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
     auto issue = [&](int st) {
         const int64_t at = (int64_t)st * P::STAGE, left = (int64_t)units * P::UNIT - at;
         const auto win = window_rsrc(stream + at, (uint32_t)max((int64_t)0, min((int64_t)P::STAGE, left)));
-        unsigned char *buf = smem + st % 3 * P::BUF;
+        unsigned char *buf = smem + st % P::DEPTH * P::BUF;
 #pragma unroll
         for (int i = 0; i < P::LOADS; ++i)
             window_to_lds16(win, buf + (i * P::THREADS + wave * 64) * 16, (uint32_t)((i * P::THREADS + tid) * 16));
@@ -191,8 +198,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
             mx_pack_tile<KS, 1>(codes, scales, n, ksteps, sets, l, members, g0 + q, p, p < members, smem + i * T::BYTES, nullptr);
         }
     } else {
-        issue(0);
-        issue(1);
+#pragma unroll
+        for (int st = 0; st < P::DEPTH - 1; ++st) issue(st);
     }
 
     // The points, and their scales as the tiles have theirs.
@@ -240,6 +247,80 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
 
     int q = 0;
     int64_t grp = g0;
+    // The end of a set group: its sums, and the maximum back to e0's.
+    auto finish = [&] {
+#pragma unroll
+        for (int i = 0; i < RT / 2; ++i) {
+            const f32x4 u = m[2 * i] + m[2 * i + 1];
+            float s = (u[0] + u[2]) + (u[1] + u[3]);
+            s += __shfl_xor(s, 16);
+            s += __shfl_xor(s, 32);
+            const int64_t part = (row0 + wave * RT * 16) / kMxSetRows + i;
+            if (g == 0 && part < parts) partials[part * lpad + grp * 16 + lr] = s;
+            m[2 * i] = m[2 * i + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        q = 0;
+        ++grp;
+    };
+    if constexpr (P::AHEAD && !GATHER) {
+        i32x4 b[KS];
+        int bs[SR];
+        float bias;
+        auto read = [&](const unsigned char *t, int ks) {
+            b[ks] = *reinterpret_cast<const i32x4 *>(t + ks * 1024 + lane * 16);
+            if (ks % 4 == 3 || ks == KS - 1) bs[ks / 4] = *reinterpret_cast<const int *>(t + T::SCALES + ks / 4 * 256 + lane * 4);
+        };
+        auto read_bias = [&](const unsigned char *t) { bias = *reinterpret_cast<const float *>(t + T::BIAS + lr * 4); };
+        // The tile at hand, and the next one's operands over those just used.
+        auto tile_then = [&](const unsigned char *next, f32x4(&acc)[RT]) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) acc[rt] = f32x4{bias, bias, bias, bias};
+            read_bias(next);
+            auto step = [&](auto kc) {
+                constexpr int ks = decltype(kc)::value;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    acc[rt] = mx_mma<ks % 4, ks % 4>(a[rt][ks], b[ks], acc[rt], as[rt][ks / 4], bs[ks / 4]);
+                read(next, ks);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            each_step(step, std::make_integer_sequence<int, KS>{});
+        };
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        read_bias(smem);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) read(smem, ks);
+        for (int st = 0; st < stages; ++st) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((P::DEPTH - 3) * P::LOADS) : "memory");  // stage st + 1
+            __syncthreads();
+            issue(st + P::DEPTH - 1);
+            const unsigned char *buf = smem + st % P::DEPTH * P::BUF, *next_buf = smem + (st + 1) % P::DEPTH * P::BUF;
+            const int last = min(ups, units - st * ups);
+            for (int u = 0; u < last; ++u) {
+                const unsigned char *t = buf + u * P::UNIT, *next = u + 1 < last ? t + P::UNIT : next_buf;
+                f32x4 x[RT], y[RT];
+                const bool two = 2 * q + 1 < members;
+                tile_then(two ? t + T::BYTES : next, x);
+                if (two) {
+                    tile_then(next, y);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) m[rt][i] = fmaxf(fmaxf(m[rt][i], x[rt][i]), y[rt][i]);
+                } else {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) m[rt][i] = fmaxf(m[rt][i], x[rt][i]);
+                }
+                if (++q == pairs) finish();
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
+        return;
+    }
     for (int st = 0; st < stages; ++st) {
         if constexpr (!GATHER) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(P::LOADS) : "memory");
         __syncthreads();
@@ -262,20 +343,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *_
 #pragma unroll
                     for (int i = 0; i < 4; ++i) m[rt][i] = fmaxf(m[rt][i], x[rt][i]);
             }
-            if (++q == pairs) {
-#pragma unroll
-                for (int i = 0; i < RT / 2; ++i) {
-                    const f32x4 u = m[2 * i] + m[2 * i + 1];
-                    float s = (u[0] + u[2]) + (u[1] + u[3]);
-                    s += __shfl_xor(s, 16);
-                    s += __shfl_xor(s, 32);
-                    const int64_t part = (row0 + wave * RT * 16) / kMxSetRows + i;
-                    if (g == 0 && part < parts) partials[part * lpad + grp * 16 + lr] = s;
-                    m[2 * i] = m[2 * i + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                }
-                q = 0;
-                ++grp;
-            }
+            if (++q == pairs) finish();
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
@@ -291,7 +359,7 @@ double mx_sets_cost(const MxSetsArgs &x, int64_t groups, int64_t *gpc) {
     using P = MxSetsPlan<KS, RT, WAVES>;
     const int64_t nrb = (x.n + P::ROWS - 1) / P::ROWS, cus = std::max<int64_t>(1, device_cu_count());
     const int64_t resident = std::min(WAVES > 4 ? 1 : RT > 2 ? 2 : 4, kLdsBytes / P::LDS);
-    const double stall = RT > 2 ? 1.0 : resident * WAVES > 4 ? 1.5 : 1.9;
+    const double stall = RT > 2 ? 1.0 : P::AHEAD ? 1.35 : resident * WAVES > 4 ? 1.5 : 1.9;
     const double group = (double)x.k * KS * RT * 16.0 * (WAVES / 4) * stall, start = 4000.0 + 500.0 * KS;
     double best = 0.0;
     for (int64_t c = 1; c <= groups; c = c < 16 ? c + 1 : c + c / 8) {
