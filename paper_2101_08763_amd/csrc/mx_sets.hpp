@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256) void mx_sets_pack_kernel(const uint8_t *__rest
 // GATHER: the workgroup makes its tiles itself, all of them at once in LDS (they
 // fit), from the sets.
 template <int KS, int RT, int WAVES, bool GATHER>
-__global__ __launch_bounds__(WAVES * 64, RT > 2 && WAVES == 4 && KS > 8 ? 1 : 2) void mx_sets_kernel(const uint8_t *__restrict__ codes,
+__global__ __launch_bounds__(WAVES * 64, 2) void mx_sets_kernel(const uint8_t *__restrict__ codes,
                                                                 const uint8_t *__restrict__ scales, int64_t n, int ksteps,
                                                                 const uint8_t *__restrict__ tiles,
                                                                 const int32_t *__restrict__ sets, int64_t l, int members,

@@ -400,6 +400,18 @@ def test_sets_do_not_depend_on_the_batch(n, d, monkeypatch):
         limit //= 2
 
 
+@pytest.mark.parametrize("n,d,l,k", [(1, 2049, 1, 1), (64, 2304, 16, 4), (65, 2304, 17, 5), (130, 4100, 33, 9),
+                                     (1000, 2176, 40, 17)])
+def test_sets_of_long_rows(n, d, l, k):
+    """Rows past the register kernels, around their blocks of points and members."""
+    q, V, sets = set_inputs(n, d, l, k)
+    s = torch.as_tensor(sets).cuda()
+    f = api.exemplar_mx_eval(q, s)
+    want = ref.f_of_sets(V, sets)
+    assert np.all(np.abs(to64(f) - want) <= 1e-5 * np.abs(want) + 1e-7 * (V * V).sum(1).mean())
+    assert torch.equal(api.exemplar_mx_eval(q, s[l - 1:].contiguous()), f[l - 1:])
+
+
 @pytest.mark.parametrize("n", [131_040, 131_041, 200_003])
 def test_sets_on_many_points(n, monkeypatch):
     """Around and past the number of partial sums that are added in two steps."""
