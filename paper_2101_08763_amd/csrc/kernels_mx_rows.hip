@@ -37,7 +37,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ 
     const uint32_t row = divide(j, per_row), c = j - row * per_row.by;
     const int d0 = (int)c * 8;
     float y[8];
-    load8(x + (int64_t)row * d + d0, d - d0, y);
+    load8<true>(x + (int64_t)row * d + d0, d - d0, y);
     const int64_t rb = (int64_t)per_row.by * BITS, rs = per_row.by / 4;
     mx_store8<BITS>(y, i < chunks, codes + row * rb, scales + row * rs, (int)c);
 }
@@ -70,7 +70,8 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t *__res
 // TPR threads share a row, chunk t + i TPR of 8 coordinates going to thread t;
 // the row stays in registers (CPT chunks a thread) between the sum of squares
 // and the result.  CPT = 0: rows too long for that, read twice.  HBM-bound:
-// 20 000 x 1 536 bf16 with a residual to 8 bits in 37 us (5.9 TB/s).
+// 20 000 x 1 536 bf16 with a residual to 8 bits in 38 us (5.6 TB/s; 45 when x and r
+// are kept in the caches, which then hold less of what is written).
 //
 // The sum and its root are held in 64 bits, and v times the root's two 32-bit
 // parts is rounded once before w's product: a row's last bit decides on which
@@ -117,10 +118,10 @@ __global__ __launch_bounds__(norm_block(TPR)) void rmsnorm_kernel(const T *x, co
     const int chunks = BITS ? (int)(mx_padded(d) / 8) : (d + 7) / 8;
     auto load = [&](int c, float(&v)[8]) {
         const int d0 = c * 8;
-        load8(x + at + d0, d - d0, v);
+        load8<(CPT > 0)>(x + at + d0, d - d0, v);
         if (r) {
             float u[8];
-            load8(r + at + d0, d - d0, u);
+            load8<(CPT > 0)>(r + at + d0, d - d0, u);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += u[e];
         }
@@ -184,7 +185,8 @@ __global__ __launch_bounds__(norm_block(TPR)) void rmsnorm_kernel(const T *x, co
 // weights and their part of dw in registers, and loads a row while it works on
 // the one before; a workgroup's parts are added in LDS in a
 // fixed order and written as one row of `partial` (grid x d).  HBM-bound: 20 000 x
-// 1 536 bf16 in 40 us (6.1 TB/s), and 4.6 for the sum of 512 parts.
+// 1 536 bf16 in 42 us (5.9 TB/s), and 4.6 for the sum of 512 parts; 47 and 4.6
+// when the rows are kept in the caches.
 // ---------------------------------------------------------------------------
 template <typename T, int TPR, int CPT>
 __global__ __launch_bounds__(256) void rmsnorm_grad_kernel(const T *__restrict__ dy, const T *__restrict__ h,
@@ -203,9 +205,9 @@ __global__ __launch_bounds__(256) void rmsnorm_grad_kernel(const T *__restrict__
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
             const int d0 = (t + i * TPR) * 8;
-            nh[i] = load8(h + at + d0, d - d0);
-            ng[i] = load8(dy + at + d0, d - d0);
-            if (dh) no[i] = load8(dh + at + d0, d - d0);
+            nh[i] = load8<true>(h + at + d0, d - d0);
+            ng[i] = load8<true>(dy + at + d0, d - d0);
+            if (dh) no[i] = load8<true>(dh + at + d0, d - d0);
         }
     };
 #pragma unroll

@@ -122,18 +122,23 @@ struct Chunk {
     typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
 };
 
-template <typename T>
+// ONCE: read once and past the caches, whose room is for what is read again.
+template <bool ONCE = false, typename T>
 __device__ __forceinline__ typename Chunk<T>::vec load8(const T *p, int have) {
-    if (have >= 8) return *reinterpret_cast<const typename Chunk<T>::vec *>(p);
+    if (have >= 8) {
+        const auto *at = reinterpret_cast<const typename Chunk<T>::vec *>(p);
+        if constexpr (ONCE) return __builtin_nontemporal_load(at);
+        return *at;
+    }
     typename Chunk<T>::vec x;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = i < have ? p[i] : (T)0.0f;
     return x;
 }
 
-template <typename T>
+template <bool ONCE = false, typename T>
 __device__ __forceinline__ void load8(const T *p, int have, float (&v)[8]) {
-    const auto x = load8(p, have);
+    const auto x = load8<ONCE>(p, have);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = to_f32((T)x[i]);
 }
