@@ -70,13 +70,14 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t *__res
 // TPR threads share a row, chunk t + i TPR of 8 coordinates going to thread t;
 // the row stays in registers (CPT chunks a thread) between the sum of squares
 // and the result.  CPT = 0: rows too long for that, read twice.  HBM-bound:
-// 20 000 x 1 536 bf16 with a residual to 8 bits in 38 us (5.6 TB/s; 45 when x and r
+// 20 000 x 1 536 bf16 with a residual to 8 bits in 40 us (5.3 TB/s; 45 when x and r
 // are kept in the caches, which then hold less of what is written).
 //
-// The sum and its root are held in 64 bits, and v times the root's two 32-bit
-// parts is rounded once before w's product: a row's last bit decides on which
-// side of a power of two a block's maximum falls, and with it the whole block's
-// scale.  It takes no time: the kernel waits for memory.
+// The sum and its root are held in 64 bits, and on the way to 8 or 4 bits y in
+// two parts, rounded to odd: a row's last bit decides on which side of a power of
+// two a block's maximum falls, and with it the whole block's scale, and rounding
+// to 24 bits first would make ties of what are none (of 31 million codes 20 came
+// out wrong).  The second part takes 2 us of these 40.
 // ---------------------------------------------------------------------------
 template <int TPR, typename S>
 __device__ __forceinline__ S row_sum(S s, S *lds) {
@@ -99,6 +100,13 @@ __device__ __forceinline__ double inverse_root(double m) {
     const double r = __builtin_amdgcn_rsq(m), half = 0.5 * r;
     const double t = fma(fma(-m * r, r, 1.0), half, r);
     return r > 0.0 && r < (double)INFINITY ? t : r;
+}
+
+// y0 + rest in 24 bits that are rounded again later: where y0 is not all of it,
+// the neighbour with an odd last bit, which no midpoint of fewer bits has.
+__device__ __forceinline__ float to_odd(float y0, float rest) {
+    const int b = __float_as_int(y0), step = (b ^ __float_as_int(rest)) >> 31 | 1;
+    return (rest > 0.0f || rest < 0.0f) && (b & 1) == 0 && b << 1 != 0 ? __int_as_float(b + step) : y0;
 }
 
 constexpr int norm_block(int tpr) { return tpr > 256 ? tpr : 256; }
@@ -137,8 +145,13 @@ __global__ __launch_bounds__(norm_block(TPR)) void rmsnorm_kernel(const T *x, co
             for (int e = 0; e < 8; ++e) g[e] = 1.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float p = v[e] * rstd, rest = fmaf(v[e], low, fmaf(v[e], rstd, -p));
-            g[e] = fmaf(p, g[e], rest * g[e]);
+            const float p = v[e] * rstd;
+            if constexpr (BITS != 0) {
+                const float rest = fmaf(v[e], low, fmaf(v[e], rstd, -p)) * g[e], y0 = fmaf(p, g[e], rest);
+                g[e] = to_odd(y0, fmaf(p, g[e], -y0) + rest);
+            } else {
+                g[e] *= p;
+            }
         }
         if constexpr (BITS != 0)
             mx_store8<BITS>(g, live && c < chunks, codes + row * mx_row_bytes(d, BITS), scales + row * mx_row_scales(d), c);

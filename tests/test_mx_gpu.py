@@ -500,6 +500,35 @@ def test_sets_past_32_bits():
     assert np.all(np.abs(got[:2] - want) <= 1e-5 * np.abs(want) + 1e-7 * norms / n)
 
 
+# -- rounding once -------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", [FP8, FP4])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_rmsnorm_rounds_once(dtype, fmt):
+    """Codes and scales are those of y in 64 bits.  Rounded to fp32 first, y would
+    be on a midpoint of the codes about once in 2^20 elements, and wrong half of
+    those times (4 to 6 of these); from both parts it is known to 2^-44."""
+    g = gen("once", str(dtype), fmt)
+    n, d = 6000, 1536
+    x, r = (torch.as_tensor(g.standard_normal((n, d))).to(dtype) for _ in range(2))
+    w = torch.as_tensor(1.0 + 0.2 * g.standard_normal(d)).to(dtype)
+    y, _, _ = api.exemplar_rmsnorm(x.cuda(), w.cuda(), r.cuda(), eps=1e-5, format=fmt)
+    want, _, _ = ref.rmsnorm(to64(x), to64(w), to64(r), float(np.float32(1e-5)))
+    codes, scales = ref.quantize(want, fmt)
+    assert np.array_equal(stored(y)[0], codes)
+    assert np.array_equal(stored(y)[1], scales)
+
+
+def test_rmsnorm_with_an_infinite_weight():
+    """It reaches its own column, or its own block, and nothing else."""
+    x, w = torch.ones(4, 64, device="cuda"), torch.ones(64, device="cuda")
+    w[3] = float("inf")
+    y, _, rstd = api.exemplar_rmsnorm(x, w, eps=0.0)
+    assert torch.equal(rstd, torch.ones(4, device="cuda")) and torch.equal(y, w.expand(4, 64))
+    q, _, _ = api.exemplar_rmsnorm(x, w, eps=0.0, format=FP8)
+    codes, scales = stored(q)
+    assert np.all(scales[:, 0] == 255) and np.all(scales[:, 1] == 127 - 8) and np.all(codes[:, 32:64] == 0x78)
+
+
 # -- together -----------------------------------------------------------------------
 def test_norm_product_and_sets_together():
     """Hidden states to scores: norm to 8 bits, projection by 4-bit weights,
