@@ -393,10 +393,9 @@ EXEMCL_API int exemplar_rmsnorm_backward(const void *dy, const void *h, const vo
  *   precision    of C: fp32, or rounded to fp16 / bf16
  *   C            device, m x n row-major; written
  *
- * Sums of 4-bit products are exact up to fp32's rounding.  With 8-bit rows and
- * fp32 results they are taken in two parts, to the same end; with 16-bit
- * results in one, whose error is about 1e-5 of the result's size, below 1/100
- * of a 16-bit rounding.  A NaN block makes its row's or column's results NaN.
+ * Sums are those of fp32, whatever the type of C: the products of 8
+ * consecutive coordinates are added exactly (of 8-bit rows in two parts), the
+ * rest with fp32's rounding, and C's type rounds once.  A NaN block makes its row's or column's results NaN.
  */
 EXEMCL_API int exemplar_mx_product(const void *A, const void *A_scales, int64_t m, int format_a, const void *B,
                                    const void *B_scales, int64_t n, int64_t d, const float *bias, int precision, void *C,

@@ -192,9 +192,10 @@ __device__ __forceinline__ f32x4 mx_mma(A a, B b, f32x4 c, int scale_a, int scal
 // with 13 bits below the largest sum of two exponents.  Those of 8-bit elements
 // are -6 .. 8, of 4-bit ones 0 .. 2, and a product has 4 bits below their sum: up
 // to 20 binades in all, but 13 among the large elements and 12 among the others.
-// So each part's sum is exact (20 000 x 1 536 against queries from N(0, 1), not
-// divided: relative error 4.5e-6, more than a sum in fp32 has; results of 16 bits
-// do without, their own rounding being 2^-9 or 2^-12).
+// So each part's sum is exact.  Results of 16 bits need it like those of 32: not
+// divided, 448 and -448 beside six elements of 0.015 leave nothing of these, and
+// with one element per 8 a hundred times the others one result in ten is off by
+// more than half a step of fp16.
 __device__ __forceinline__ void mx_divide(i32x8 x, i32x8 &high, i32x8 &low) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

@@ -18,7 +18,7 @@ namespace exemcl {
 // us (2.4 TB/s), a launch and the wait for three loads in turn.
 constexpr int kDirectWaves = 4;
 
-template <typename T, int BITS_A, bool DIVIDE>
+template <typename T, int BITS_A>
 __global__ __launch_bounds__(kDirectWaves * 64) void mx_product_direct_kernel(
     const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, int64_t m, const uint8_t *__restrict__ B,
     const uint8_t *__restrict__ Bs, int64_t n, int64_t d, int64_t ntiles, const float *__restrict__ bias,
@@ -40,14 +40,10 @@ __global__ __launch_bounds__(kDirectWaves * 64) void mx_product_direct_kernel(
         } else {
             const i32x8 a = mx_join(*reinterpret_cast<const i32x4 *>(a_row + ks * 128 + g * 16),
                                     *reinterpret_cast<const i32x4 *>(a_row + ks * 128 + 64 + g * 16));
-            if constexpr (DIVIDE) {
-                i32x8 high, low;
-                mx_divide(a, high, low);
-                acc = mx_mma(b, low, acc, sb, sa);
-                acc = mx_mma(b, high, acc, sb, sa);
-            } else {
-                acc = mx_mma(b, a, acc, sb, sa);
-            }
+            i32x8 high, low;
+            mx_divide(a, high, low);
+            acc = mx_mma(b, low, acc, sb, sa);
+            acc = mx_mma(b, high, acc, sb, sa);
         }
     }
     sums[wave][lane] = acc;
@@ -76,11 +72,11 @@ __global__ __launch_bounds__(kDirectWaves * 64) void mx_product_direct_kernel(
 // own order, takes the address units 64 steps a load instead of 16: 16 384 x
 // 8 192 x 4 096 565 us).
 //
-// That size, 8 by 4 bits to bf16, takes 416 us (2.65 PFLOP/s; the instruction
-// alone, on random values, runs at 4.2), 4 by 4 bits 303 (3.6 of 6.8).  With zeros
-// for data it is 385: on others the chip lowers its clock.  The rest is the start
-// and the end of a tile, LDS reads and copies between instructions: wavefronts of
-// 128 x 128, 128 x 64 or 64 x 128 end within 3 % of each other.
+// That size, 8 by 4 bits to bf16, takes 654 us: two instructions for every 128
+// coordinates (mx_divide), together at 3.4 PFLOP/s where the instruction alone, on
+// random values, runs at 4.2.  4 by 4 bits takes 312 (3.5 of 6.8).  The rest is the
+// start and the end of a tile, LDS reads and copies between instructions, and the
+// clock, which the chip lowers on random values.
 // ---------------------------------------------------------------------------
 template <int BITS_A, int WM, int NB, int PM, int PN, int DEPTH>
 struct MxTilePlan {
@@ -104,7 +100,7 @@ struct MxTilePlan {
     static_assert(A_FRAGS % WAVES == 0 && B_FRAGS % WAVES == 0 && BM % 64 == 0 && LDS <= kLdsBytes, "geometry");
 };
 
-template <typename T, int BITS_A, bool DIVIDE, int WM, int NB, int PM, int PN, int DEPTH>
+template <typename T, int BITS_A, int WM, int NB, int PM, int PN, int DEPTH>
 __global__ __launch_bounds__(PM *PN * 64, 2) void mx_product_kernel(
     const uint8_t *__restrict__ A, const uint8_t *__restrict__ As, int64_t m, const uint8_t *__restrict__ B,
     const uint8_t *__restrict__ Bs, int64_t n, int ksteps, int mblocks, int nblocks, const float *__restrict__ bias,
@@ -271,23 +267,14 @@ __global__ __launch_bounds__(PM *PN * 64, 2) void mx_product_kernel(
                     if (w == WM - 1) read_b(x, j);
                 }
             } else {
-                const i32x8 ax = mx_join(a[w][0], a[w][1]);
-                if constexpr (DIVIDE) {
-                    i32x8 high, low;
-                    mx_divide(ax, high, low);
+                i32x8 high, low;
+                mx_divide(mx_join(a[w][0], a[w][1]), high, low);
 #pragma unroll
-                    for (int j = 0; j < WN; ++j) acc[w][j] = mx_mma(b[j], low, acc[w][j], bs[j], as[w]);
+                for (int j = 0; j < WN; ++j) acc[w][j] = mx_mma(b[j], low, acc[w][j], bs[j], as[w]);
 #pragma unroll
-                    for (int j = 0; j < WN; ++j) {
-                        acc[w][j] = mx_mma(b[j], high, acc[w][j], bs[j], as[w]);
-                        if (w == WM - 1) read_b(x, j);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < WN; ++j) {
-                        acc[w][j] = mx_mma(b[j], ax, acc[w][j], bs[j], as[w]);
-                        if (w == WM - 1) read_b(x, j);
-                    }
+                for (int j = 0; j < WN; ++j) {
+                    acc[w][j] = mx_mma(b[j], high, acc[w][j], bs[j], as[w]);
+                    if (w == WM - 1) read_b(x, j);
                 }
             }
             // Reads and copies between the instructions: all at once, they hold
@@ -388,20 +375,20 @@ __global__ __launch_bounds__(PM *PN * 64, 2) void mx_product_kernel(
     }
 }
 
-template <typename T, int BITS_A, bool DIVIDE>
+template <typename T, int BITS_A>
 hipError_t product_direct(const MxProductArgs &a, hipStream_t st) {
     const int64_t mt = (a.m + 15) / 16, nt = (a.n + 15) / 16;
     if (mt > (int64_t(1) << 34) / nt) return hipErrorInvalidValue;  // 2^14 rows of kFlatRow
-    hipLaunchKernelGGL((mx_product_direct_kernel<T, BITS_A, DIVIDE>), flat_grid(mt * nt, kDirectWaves * 64),
+    hipLaunchKernelGGL((mx_product_direct_kernel<T, BITS_A>), flat_grid(mt * nt, kDirectWaves * 64),
                        dim3(kDirectWaves * 64), 0, st, (const uint8_t *)a.A, (const uint8_t *)a.A_scales, a.m,
                        (const uint8_t *)a.B, (const uint8_t *)a.B_scales, a.n, a.d, nt, a.bias, (T *)a.C);
     return hipGetLastError();
 }
 
-template <typename T, int BITS_A, bool DIVIDE, int WM, int NB, int PM, int PN, int DEPTH>
+template <typename T, int BITS_A, int WM, int NB, int PM, int PN, int DEPTH>
 hipError_t product_tiled(const MxProductArgs &a, hipStream_t st) {
     using P = MxTilePlan<BITS_A, WM, NB, PM, PN, DEPTH>;
-    auto kern = mx_product_kernel<T, BITS_A, DIVIDE, WM, NB, PM, PN, DEPTH>;
+    auto kern = mx_product_kernel<T, BITS_A, WM, NB, PM, PN, DEPTH>;
     static std::atomic<bool> ready[kMaxDevices];  // the attribute holds for one device
     const int dev = current_device();
     if (dev < 0) return hipErrorInvalidDevice;
@@ -420,48 +407,51 @@ hipError_t product_tiled(const MxProductArgs &a, hipStream_t st) {
 
 // The kernel for a size.  Where a tile of 64 x 128 leaves most CUs without one,
 // 16 x 16 tiles with the coordinates dealt out to four wavefronts; else the
-// largest tile that still makes enough of them (us, 8 by 4 bits to bf16):
-//                          16x16  64x128  128x128  128x256  256x256
-//   24 x 2 000 x 1 024       4.2     8.5      9.0     12.8     19.4
-//   130 x 8 192 x 1 024     25.1    10.3     11.0     14.9     20.5
-//   1 024 x 8 192 x 1 024            22.6     16.9     18.7     23.8
-//   1 024 x 30 000 x 1 024           64.4     47.8     42.8     48.2
-//   16 384 x 8 192 x 1 024                   157      130      153
-//   16 384 x 8 192 x 4 096                   491      424      416
-// The largest has one workgroup per CU, which starts and ends alone: it wins
-// from about 3 000 coordinates on (1 500 with 4-bit rows), where its last round is
-// full.  Rows in two parts take 128 x 256: two workgroups per CU cover the
-// division (16 384 x 8 192 x 4 096 to fp32: 711 us, the largest 890).
+// largest tile that still makes enough of them (us, to bf16; 8 and 4: bits of A):
+//                            16x16  64x128  128x128  128x256  256x256
+//   24 x 2 000 x 1 024     8   3.7    12.1     12.6     17.4
+//                          4   3.4     7.2      7.3     10.6
+//   130 x 8 192 x 1 024    8  23.3    12.6     13.2     18.7     30.0
+//                          4  19.6     7.6      8.5     12.3     12.8
+//   1 024 x 8 192 x 1 024  8          32.9     20.7     21.0     32.3
+//                          4          16.3     12.3     14.7     16.1
+//   1 024 x 30 000 x 1 024 8         102       68.5     56.4     70.3
+//                          4          50.6     38.4     39.9     40.8
+//   16 384 x 8 192 x 1 024 8         407      247      188      253
+//                          4         163      116      123      129
+//   16 384 x 8 192 x 4 096 8        1394      818      654      805
+//                          4         506      408      354      312
+// The largest has one workgroup per CU, which starts and ends alone: with 4-bit
+// rows it wins from about 1 500 coordinates on, where its last round is full; with
+// 8-bit rows two workgroups per CU cover the division, and it never does.
 // Stores of fp32 results overlap less of what follows them, and 128 x 256 pays
-// earlier (333 x 30 011 x 301, 2.75 tiles of 128 x 128 a CU: 21.4 us instead of
-// 23.5).  With 4-bit rows two stages are enough for 128 x 128 and let three
-// workgroups share a CU (the same to bf16: 12.4 us instead of 15.4).
-template <typename T, int BITS_A, bool DIVIDE>
+// earlier (333 x 30 011 x 301 of 8 bits, 2.75 tiles of 128 x 128 a CU: 21.2 us
+// instead of 22.9).  With 4-bit rows two stages are enough for 128 x 128 and let
+// three workgroups share a CU (the same to bf16: 12.8 us instead of 16.2).
+template <typename T, int BITS_A>
 hipError_t product_run(const MxProductArgs &a, hipStream_t st) {
     const int64_t cus = std::max<int64_t>(1, device_cu_count());
     auto tiles = [&](int64_t bm, int64_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
     const double ks = (double)(mx_padded(a.d) / kMxRow);
     // us, fitted to 8 to 4 096 x 300 to 30 000 x 256 to 4 096
     const double direct = 3.2 + 0.1 * ks + (BITS_A == 8 ? 5e-4 : 4e-4) * (double)tiles(16, 16) * (ks + 0.5);
-    const double tiled = 5.4 + (DIVIDE ? 0.9 : BITS_A == 8 ? 0.38 : 0.3) * ks;
-    if (direct <= tiled * std::max(1.0, (double)tiles(64, 128) / (2.0 * cus))) return product_direct<T, BITS_A, DIVIDE>(a, st);
-    if (tiles(64, 128) <= cus) return product_tiled<T, BITS_A, DIVIDE, 4, 1, 1, 2, 3>(a, st);
+    const double tiled = 5.4 + (BITS_A == 8 ? 0.9 : 0.3) * ks;
+    if (direct <= tiled * std::max(1.0, (double)tiles(64, 128) / (2.0 * cus))) return product_direct<T, BITS_A>(a, st);
+    if (tiles(64, 128) <= cus) return product_tiled<T, BITS_A, 4, 1, 1, 2, 3>(a, st);
     if (tiles(128, 128) * 2 <= (sizeof(T) == 4 ? 5 : 6) * cus)
-        return product_tiled<T, BITS_A, DIVIDE, 4, 1, 2, 2, BITS_A == 8 ? 3 : 2>(a, st);
-    const int64_t large = tiles(256, 256), last = (large + cus - 1) / cus * cus;
-    if constexpr (!DIVIDE)
-        if (ks >= (BITS_A == 8 ? 24 : 12) && last * 10 <= large * 11)
-            return product_tiled<T, BITS_A, DIVIDE, 8, 1, 2, 4, 3>(a, st);
-    return product_tiled<T, BITS_A, DIVIDE, 4, 2, 2, 2, 2>(a, st);
+        return product_tiled<T, BITS_A, 4, 1, 2, 2, BITS_A == 8 ? 3 : 2>(a, st);
+    if constexpr (BITS_A == 4) {
+        const int64_t large = tiles(256, 256), last = (large + cus - 1) / cus * cus;
+        if (ks >= 12 && last * 10 <= large * 11) return product_tiled<T, BITS_A, 8, 1, 2, 4, 3>(a, st);
+    }
+    return product_tiled<T, BITS_A, 4, 2, 2, 2, 2>(a, st);
 }
 
-// DIVIDE: 8-bit rows in two parts (mx_divide), for results in fp32; what the
-// matrix cores drop otherwise is far below the rounding of a 16-bit result.
 template <int BITS_A>
 hipError_t product_typed(int prec, const MxProductArgs &a, hipStream_t st) {
-    if (prec == P_FP32) return product_run<float, BITS_A, BITS_A == 8>(a, st);
-    if (prec == P_FP16) return product_run<_Float16, BITS_A, false>(a, st);
-    return product_run<__bf16, BITS_A, false>(a, st);
+    if (prec == P_FP32) return product_run<float, BITS_A>(a, st);
+    if (prec == P_FP16) return product_run<_Float16, BITS_A>(a, st);
+    return product_run<__bf16, BITS_A>(a, st);
 }
 
 }  // namespace exemcl
