@@ -153,10 +153,14 @@ __global__ __launch_bounds__(norm_block(TPR)) void rmsnorm_kernel(const T *x, co
                 g[e] *= p;
             }
         }
-        if constexpr (BITS != 0)
+        if constexpr (BITS != 0) {
+            if (d - d0 < 8)  // past d: zeros, where 0 rstd is not
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] = e < d - d0 ? g[e] : 0.0f;
             mx_store8<BITS>(g, live && c < chunks, codes + row * mx_row_bytes(d, BITS), scales + row * mx_row_scales(d), c);
-        else if (live)
+        } else if (live) {
             store8(y + at + d0, d - d0, g);
+        }
     };
     double s = 0.0;
     if constexpr (CPT > 0) {
