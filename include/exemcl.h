@@ -344,7 +344,8 @@ EXEMCL_API int exemplar_mx_dequantize(const void *codes, const void *scales, int
  * exemplar_rmsnorm -- root-mean-square norm of n rows, with the residual's
  * addition before it and the rounding to microscaled rows behind it:
  *   v = x + residual,  y = v * weight / sqrt(mean(v^2) + eps).
- * v is in fp32 and not rounded again, the mean and its root are in fp64.
+ * v is in fp32 and not rounded again, the mean and its root are in fp64.  A y past
+ * fp32's range is infinite (and its block NaN).
  *
  *   x, residual  device, n x d row-major, type per `precision`; residual may be
  *                NULL (v = x)

@@ -103,10 +103,12 @@ __device__ __forceinline__ double inverse_root(double m) {
 }
 
 // y0 + rest in 24 bits that are rounded again later: where y0 is not all of it,
-// the neighbour with an odd last bit, which no midpoint of fewer bits has.
+// the neighbour with an odd last bit, which no midpoint of fewer bits has.  Of a y0
+// that is infinite the rest is too, or NaN, and it stays.
 __device__ __forceinline__ float to_odd(float y0, float rest) {
     const int b = __float_as_int(y0), step = (b ^ __float_as_int(rest)) >> 31 | 1;
-    return (rest > 0.0f || rest < 0.0f) && (b & 1) == 0 && b << 1 != 0 ? __int_as_float(b + step) : y0;
+    constexpr int finite = 0x198;  // normal or subnormal, of either sign
+    return __builtin_amdgcn_classf(rest, finite) && (b & 1) == 0 && b << 1 != 0 ? __int_as_float(b + step) : y0;
 }
 
 constexpr int norm_block(int tpr) { return tpr > 256 ? tpr : 256; }
