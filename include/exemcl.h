@@ -302,7 +302,8 @@ EXEMCL_API int exemplar_sqnorm(const void *V, int64_t n, int64_t d, int precisio
  * where a call says so.  Outputs must not overlap inputs unless a call says
  * that they may.  exemplar_rmsnorm_backward with dweight and exemplar_mx_eval
  * take temporary memory as exemplar_eval does, so they are not for code under
- * HIP graph capture; the others take none and may be captured.
+ * HIP graph capture: on a capturing stream they return EINVAL and queue nothing.
+ * The others take none and may be captured.
  * ------------------------------------------------------------------------ */
 enum exemcl_mx_format {
     EXEMCL_MX_NONE = 0, /* exemplar_rmsnorm only: rows of the input's type */

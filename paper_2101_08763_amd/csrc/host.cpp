@@ -849,6 +849,21 @@ int scratch_arena(Arena *a) {
     return EXEMCL_OK;
 }
 
+// Temporary memory within the limit, for a stream that is not being captured.  A
+// block allocated under capture belongs to the graph and is gone with it, and a
+// kept one may be released before the graph is: neither is for kernels that a
+// graph replays.
+int alloc_uncaptured(Scratch *s, int64_t bytes, int64_t limit, hipStream_t st) {
+    if (bytes > limit) return EXEMCL_ENOMEM;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(st, &status) != hipSuccess) {
+        (void)hipGetLastError();
+        return EXEMCL_EDEVICE;
+    }
+    if (status != hipStreamCaptureStatusNone) return EXEMCL_EINVAL;
+    return alloc_scratch(s, bytes, st);
+}
+
 // f of l sets of k 4-bit rows, in chunks of whole set groups where the
 // temporary memory for all of them is not to be had (as in run_eval).
 int run_mx_eval(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets, int64_t l, int64_t k,
@@ -862,7 +877,7 @@ int run_mx_eval(const void *codes, const void *scales, int64_t n, int64_t d, con
         lpad = align_up(lc, unit);
         off = align_up(lpad / unit * mx_sets_work(d, k), 256);
         const int64_t bytes = off + (G + folds) * lpad * 4;
-        const int rc = bytes <= limit ? alloc_scratch(&ws, bytes, st) : EXEMCL_ENOMEM;
+        const int rc = alloc_uncaptured(&ws, bytes, limit, st);
         if (rc == EXEMCL_OK) break;
         if (rc != EXEMCL_ENOMEM || lc <= unit) return rc;
         lc = align_up((lc + 1) / 2, unit);
@@ -1226,9 +1241,7 @@ EXEMCL_API int exemplar_rmsnorm_backward(const void *dy, const void *h, const vo
     NormGradArgs a{dy, h, weight, rstd, dh, n, d, rmsnorm_grad_parts(n, d), dx, dweight, nullptr};
     Scratch ws;
     if (dweight) {
-        const int64_t bytes = a.parts * d * 4;
-        if (bytes > workspace_limit()) return EXEMCL_ENOMEM;
-        const int rc = alloc_scratch(&ws, bytes, st);
+        const int rc = alloc_uncaptured(&ws, a.parts * d * 4, workspace_limit(), st);
         if (rc) return rc;
         a.partial = (float *)ws.ptr;
     }
