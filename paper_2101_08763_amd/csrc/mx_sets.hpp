@@ -38,6 +38,9 @@ namespace exemcl {
 constexpr int kMxSetRows = 32;        // points per partial sum
 constexpr int64_t kMxSetsD = 2048;    // longest rows kept in registers
 constexpr int64_t kMxGatherUnits = 8; // pairs of members a workgroup stages itself
+// Members of a set, and pairs of members a workgroup goes through, that the
+// kernels count in 32 bits (the tiles of one group of so many take a terabyte).
+constexpr int64_t kMxMembers = int64_t(1) << 30;
 
 // Arguments of one launch: tiles (or biases) go to `work`.
 struct MxSetsArgs {
@@ -361,8 +364,9 @@ double mx_sets_cost(const MxSetsArgs &x, int64_t groups, int64_t *gpc) {
     const int64_t resident = std::min(WAVES > 4 ? 1 : RT > 2 ? 2 : 4, kLdsBytes / P::LDS);
     const double stall = RT > 2 ? 1.0 : P::AHEAD ? 1.35 : resident * WAVES > 4 ? 1.5 : 1.9;
     const double group = (double)x.k * KS * RT * 16.0 * (WAVES / 4) * stall, start = 4000.0 + 500.0 * KS;
+    const int64_t most = std::min(groups, std::max<int64_t>(1, kMxMembers / ((x.k + 1) / 2)));
     double best = 0.0;
-    for (int64_t c = 1; c <= groups; c = c < 16 ? c + 1 : c + c / 8) {
+    for (int64_t c = 1; c <= most; c = c < 16 ? c + 1 : c + c / 8) {
         const int64_t wgs = nrb * ((groups + c - 1) / c), each = std::min(resident, (wgs + cus - 1) / cus);
         const int64_t rounds = (wgs + cus * resident - 1) / (cus * resident);
         const double cost = (double)rounds * ((double)(c * each) * group + start);
@@ -384,7 +388,6 @@ hipError_t mx_sets_launch(const MxSetsArgs &x, int64_t groups, int64_t gpc, hipS
         ready[dev].store(true, std::memory_order_release);
     }
     const int64_t nrb = (x.n + P::ROWS - 1) / P::ROWS;
-    if (gpc * ((x.k + 1) / 2) > (1 << 30)) return hipErrorInvalidValue;
     hipLaunchKernelGGL(kern, flat_grid(nrb * ((groups + gpc - 1) / gpc), P::THREADS), dim3(P::THREADS), P::LDS, st, x.codes,
                        x.scales, x.n, (int)(mx_padded(x.d) / kMxRow), x.work, x.sets, x.l, (int)x.k, (int)groups, (int)gpc,
                        (int)nrb, x.partials, x.lpad);
@@ -396,7 +399,7 @@ hipError_t mx_sets_launch(const MxSetsArgs &x, int64_t groups, int64_t gpc, hipS
 template <int KS, int RT, int WAVES>
 hipError_t mx_sets_run(const MxSetsArgs &x, hipStream_t st) {
     const int64_t groups = x.lpad / 16, slots = (x.k + 1) / 2 * 2, ntiles = groups * slots;
-    if (x.k > (1 << 24) || groups > INT32_MAX) return hipErrorInvalidValue;
+    if (x.k > kMxMembers || groups > INT32_MAX) return hipErrorInvalidValue;
     int64_t gpc = 1, gpc2 = 1;
     const bool large = mx_sets_cost<KS, RT, WAVES>(x, groups, &gpc) <= mx_sets_cost<KS, 2, 4>(x, groups, &gpc2);
     // Few short tiles: each workgroup makes its own, which saves the launch that

@@ -58,9 +58,25 @@ static void check_capture() {
     }
 }
 
+// Sets of any size, as exemplar_eval takes them: the count of members is 64 bits,
+// and the tiles of one group of 16 sets bound it through their memory alone.
+static void check_members() {
+    for (int64_t d : {20, 300, 1536, 2048, 2500})
+        for (int64_t k : {int64_t(1) << 24, (int64_t(1) << 24) + 1, int64_t(40000000), int64_t(1) << 28})
+            for (int64_t l : {1, 40, 100}) {
+                const std::string at = "d " + std::to_string(d) + " k " + std::to_string(k) + " l " + std::to_string(l);
+                expect(eval(1000, d, l, k, fresh_stream()) == EXEMCL_OK, "members", at);
+                const size_t left = fake::pool_left;
+                fake::pool_left = size_t(1) << 20;
+                expect(eval(1000, d, l, k, fresh_stream()) == EXEMCL_ENOMEM, "no memory for one group", at);
+                fake::pool_left = left;
+            }
+}
+
 int main(int argc, char **argv) {
     const std::string what = argc > 1 ? argv[1] : "";
     if (what == "capture") check_capture();
+    else if (what == "members") check_members();
     else expect(false, "no such check", what);
     if (failures) fprintf(stderr, "%d checks failed\n", failures);
     else printf("%s: checks passed\n", what.c_str());

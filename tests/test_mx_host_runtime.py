@@ -35,7 +35,7 @@ def run(driver, *args, stdin=""):
     return subprocess.run([driver, *args], input=stdin, capture_output=True, text=True, timeout=300, env=env)
 
 
-@pytest.mark.parametrize("check", ["capture"])
+@pytest.mark.parametrize("check", ["capture", "members"])
 def test_host_runtime(driver, check):
     r = run(driver, check)
     assert r.returncode == 0 and "checks passed" in r.stdout, r.stdout + r.stderr
