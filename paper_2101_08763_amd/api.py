@@ -1,9 +1,11 @@
 """Python binding of the C ABI in include/exemcl.h (argument marshalling only).
 
 Every function takes torch tensors that already live on the current HIP
-device, passes their device pointers and the current torch stream to
-libexemcl.so, and returns without synchronising.  No computation happens
-here; when the library is missing every call raises.
+device, passes their device pointers and the current torch stream (or the one
+given as ``stream``) to libexemcl.so, and returns without synchronising.  On
+a given stream the caller orders the call behind what writes its inputs, and
+what reads its results behind the call; their memory may be freed at any time.
+No computation happens here; when the library is missing every call raises.
 """
 from __future__ import annotations
 
@@ -121,6 +123,47 @@ def _stream(stream):
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _torch_stream(stream):
+    import torch
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)
+
+
+def _empty_on(stream):
+    """torch.empty and empty_like for what a call on ``stream`` writes.  PyTorch's
+    allocator hands out memory whose last use is still queued on the stream it
+    belongs to, so a result of another stream comes from that one's memory, and is
+    not reused there before the current stream, which gets it, is done with it."""
+    import torch
+    st = _torch_stream(stream)
+
+    def empty(shape, dtype, device):
+        if device.type != "cuda":
+            return torch.empty(shape, dtype=dtype, device=device)
+        with torch.cuda.stream(st):
+            t = torch.empty(shape, dtype=dtype, device=device)
+        t.record_stream(torch.cuda.current_stream(device))
+        return t
+
+    return empty, lambda t: empty(t.shape, t.dtype, t.device)
+
+
+def _empty(stream):
+    """torch.empty for results of a call on ``stream`` (None: the current one)."""
+    import torch
+    return torch.empty if stream is None else _empty_on(stream)[0]
+
+
+def _used(stream, *tensors):
+    """Keeps the memory of a call's tensors, when they are freed early, until
+    the ``stream`` it was given is done with them."""
+    if stream is None:
+        return
+    st = _torch_stream(stream)
+    for t in tensors:
+        if t is not None and t.is_cuda:
+            t.record_stream(st)
+
+
 def _check_device(*tensors):
     dev = None
     for t in tensors:
@@ -162,11 +205,12 @@ def exemplar_eval(V, sets, out=None, stream=None):
     n, d = V.shape
     l, k = sets.shape
     if out is None:
-        out = torch.empty(l, dtype=torch.float32, device=V.device)
+        out = _empty(stream)(l, dtype=torch.float32, device=V.device)
     elif out.dtype != torch.float32 or out.numel() != l:
         raise ValueError("out must be float32 with l elements")
     with _device_scope(_check_device(V, sets, out)):
         rc = load().exemplar_eval(_ptr(V), n, d, _ptr(sets), l, k, prec, _ptr(out), _stream(stream))
+    _used(stream, V, sets, out)
     if rc != EXEMCL_OK:
         raise ExemclError(rc, "exemplar_eval")
     return out
@@ -189,6 +233,7 @@ def exemplar_eval_noalloc(V, sets, out, stream=None):
         raise ValueError("out must be float32 with l elements")
     with _device_scope(_check_device(V, sets, out)):
         rc = load().exemplar_eval_noalloc(_ptr(V), n, d, _ptr(sets), l, k, prec, _ptr(out), _stream(stream))
+    _used(stream, V, sets, out)
     if rc != EXEMCL_OK:
         raise ExemclError(rc, "exemplar_eval_noalloc")
     return out
@@ -236,12 +281,13 @@ def exemplar_gain(V, S, cands, out=None, stream=None):
     n, d = V.shape
     l = cands.numel()
     if out is None:
-        out = torch.empty(l, dtype=torch.float32, device=V.device)
+        out = _empty(stream)(l, dtype=torch.float32, device=V.device)
     elif out.dtype != torch.float32 or out.numel() != l:
         raise ValueError("out must be float32 with one element per candidate")
     with _device_scope(_check_device(V, S if S.numel() else None, cands, out)):
         rc = load().exemplar_gain(_ptr(V), n, d, _ptr(S), S.numel(), _ptr(cands), l, _ptr(out),
                                   _stream(stream))
+    _used(stream, V, S, cands, out)
     if rc != EXEMCL_OK:
         raise ExemclError(rc, "exemplar_gain")
     return out
@@ -259,13 +305,14 @@ def exemplar_greedy(V, K, S_out=None, f_out=None, stream=None):
     n, d = V.shape
     K = int(K)
     if S_out is None:
-        S_out = torch.empty(max(K, 0), dtype=torch.int32, device=V.device)
+        S_out = _empty(stream)(max(K, 0), dtype=torch.int32, device=V.device)
     if f_out is None:
-        f_out = torch.empty(max(K, 0), dtype=torch.float32, device=V.device)
+        f_out = _empty(stream)(max(K, 0), dtype=torch.float32, device=V.device)
     if S_out.dtype != torch.int32 or f_out.dtype != torch.float32 or S_out.numel() < K or f_out.numel() < K:
         raise ValueError("S_out must be int32 and f_out float32, with K elements each")
     with _device_scope(_check_device(V, S_out if K > 0 else None, f_out if K > 0 else None)):
         rc = load().exemplar_greedy(_ptr(V), n, d, K, _ptr(S_out), _ptr(f_out), _stream(stream))
+    _used(stream, V, S_out, f_out)
     if rc != EXEMCL_OK:
         raise ExemclError(rc, "exemplar_greedy")
     return S_out, f_out
@@ -277,11 +324,12 @@ def exemplar_sqnorm(V, out=None, stream=None):
     prec = precision_of(V.dtype)
     n, d = V.shape
     if out is None:
-        out = torch.empty(n, dtype=torch.float32, device=V.device)
+        out = _empty(stream)(n, dtype=torch.float32, device=V.device)
     elif out.dtype != torch.float32 or out.numel() != n:
         raise ValueError("out must be float32 with n elements")
     with _device_scope(_check_device(V, out)):
         rc = load().exemplar_sqnorm(_ptr(V), n, d, prec, _ptr(out), _stream(stream))
+    _used(stream, V, out)
     if rc != EXEMCL_OK:
         raise ExemclError(rc, "exemplar_sqnorm")
     return out
@@ -332,11 +380,11 @@ def _mx_check(q, name):
     return n
 
 
-def _mx_empty(n, d, format, device):
+def _mx_empty(n, d, format, device, empty):
     import torch
     rb, rs = _mx_row(d, format)
-    return MxRows(torch.empty((n, rb), dtype=torch.uint8, device=device),
-                  torch.empty((n, rs), dtype=torch.uint8, device=device), d, format)
+    return MxRows(empty((n, rb), dtype=torch.uint8, device=device),
+                  empty((n, rs), dtype=torch.uint8, device=device), d, format)
 
 
 def _run(name, tensors, stream, *args):
@@ -355,6 +403,8 @@ def _run(name, tensors, stream, *args):
     else:
         with torch.cuda.device(dev):
             rc = fn(*args, _stream(stream))
+    if stream is not None:
+        _used(stream, *tensors)
     if rc != EXEMCL_OK:
         raise ExemclError(rc, name)
 
@@ -381,7 +431,7 @@ def exemplar_mx_quantize(x, format, out=None, stream=None):
     prec = _precision(x.dtype)
     n, d = x.shape
     if out is None:
-        out = _mx_empty(n, d, format, x.device)
+        out = _mx_empty(n, d, format, x.device, _empty(stream))
     elif out.d != d or out.format != format or _mx_check(out, "out") != n:
         raise ValueError("out must be MxRows of x's shape and the format")
     codes, scales = out.codes, out.scales
@@ -393,12 +443,11 @@ def exemplar_mx_quantize(x, format, out=None, stream=None):
 def exemplar_mx_dequantize(q, dtype, out=None, stream=None):
     """The values of MxRows q as an n x d tensor of ``dtype`` (see
     exemplar_mx_dequantize in exemcl.h)."""
-    import torch
     prec = _precision(dtype)
     n = _mx_check(q, "q")
     codes, scales, d, format = q
     if out is None:
-        out = torch.empty((n, d), dtype=dtype, device=codes.device)
+        out = _empty(stream)((n, d), dtype=dtype, device=codes.device)
     elif out.dtype != dtype or out.shape != (n, d):
         raise ValueError("out must be an n x d tensor of the dtype")
     _run("exemplar_mx_dequantize", (codes, scales, out), stream, codes.data_ptr(), scales.data_ptr(), n, d, format, prec,
@@ -421,13 +470,14 @@ def exemplar_rmsnorm(x, weight=None, residual=None, eps=1e-6, format=None, strea
         raise ValueError("weight must have x's type and d elements")
     if residual is not None and (residual.dtype != dtype or residual.shape != x.shape):
         raise ValueError("residual must have x's type and shape")
-    rstd = torch.empty(n, dtype=torch.float32, device=device)
-    h = x if residual is None else torch.empty_like(residual)
+    empty, like = (torch.empty, torch.empty_like) if stream is None else _empty_on(stream)
+    rstd = empty(n, dtype=torch.float32, device=device)
+    h = x if residual is None else like(residual)
     if format is None or format == EXEMCL_MX_NONE:
-        y = codes = torch.empty_like(x)
+        y = codes = like(x)
         scales, format = None, EXEMCL_MX_NONE
     else:
-        y = _mx_empty(n, d, format, device)
+        y = _mx_empty(n, d, format, device, empty)
         codes, scales = y.codes, y.scales
     _run("exemplar_rmsnorm", (x, residual, weight), stream, x.data_ptr(), _at(residual), _at(weight), n, d, prec, eps,
          format, None if residual is None else h.data_ptr(), codes.data_ptr(), _at(scales), rstd.data_ptr())
@@ -452,8 +502,9 @@ def exemplar_rmsnorm_backward(dy, h, weight, rstd, dh=None, stream=None):
         raise ValueError("weight must have h's type and d elements")
     if rstd.dtype != torch.float32 or rstd.shape != (n,):
         raise ValueError("rstd must be float32 with n elements")
-    dx = torch.empty_like(h)
-    dw = torch.empty(d, dtype=torch.float32, device=h.device)
+    empty, like = (torch.empty, torch.empty_like) if stream is None else _empty_on(stream)
+    dx = like(h)
+    dw = empty(d, dtype=torch.float32, device=h.device)
     _run("exemplar_rmsnorm_backward", (h, dy, weight, rstd, dh), stream, dy.data_ptr(), h.data_ptr(), _at(weight),
          rstd.data_ptr(), _at(dh), n, d, prec, dx.data_ptr(), dw.data_ptr())
     return dx, dw
@@ -476,7 +527,7 @@ def exemplar_mx_product(A, B, bias=None, dtype=None, out=None, stream=None):
     if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,)):
         raise ValueError("bias must be float32 with one element per row of B")
     if out is None:
-        out = torch.empty((m, n), dtype=dtype, device=a.device)
+        out = _empty(stream)((m, n), dtype=dtype, device=a.device)
     elif out.dtype != dtype or out.shape != (m, n):
         raise ValueError("out must be an m x n tensor of the dtype")
     _run("exemplar_mx_product", (a, a_scales, b, b_scales, bias, out), stream, a.data_ptr(), a_scales.data_ptr(), m, format,
@@ -498,7 +549,7 @@ def exemplar_mx_eval(V, sets, out=None, stream=None):
         raise TypeError("sets must be int32")
     l, k = sets.shape
     if out is None:
-        out = torch.empty(l, dtype=torch.float32, device=codes.device)
+        out = _empty(stream)(l, dtype=torch.float32, device=codes.device)
     elif out.dtype != torch.float32 or out.numel() != l:
         raise ValueError("out must be float32 with l elements")
     _run("exemplar_mx_eval", (codes, scales, sets, out), stream, codes.data_ptr(), scales.data_ptr(), n, d, sets.data_ptr(),
