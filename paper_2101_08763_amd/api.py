@@ -387,6 +387,15 @@ def _mx_empty(n, d, format, device, empty):
                   empty((n, rs), dtype=torch.uint8, device=device), d, format)
 
 
+def _check_gradient(name, tensors):
+    """Results carry no autograd graph: a gradient that is asked for would be lost
+    without a word.  (Codes of rows have none to lose.)"""
+    import torch
+    if name != "exemplar_mx_quantize" and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{name} records no gradient: call it under torch.no_grad() or on detached tensors "
+                         "(exemplar_rmsnorm_backward computes the norm's)")
+
+
 def _run(name, tensors, stream, *args):
     """Call ``name`` of the library on the device of ``tensors`` (the first
     one's; None: not given) with ``args`` and the stream, and raise its error.
@@ -395,7 +404,8 @@ def _run(name, tensors, stream, *args):
     import torch
     dev = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (dev < 0 or t.get_device() != dev or not t.is_contiguous()):
+        if t is not None and (dev < 0 or t.get_device() != dev or not t.is_contiguous() or t.requires_grad):
+            _check_gradient(name, tensors)
             _check_device(*tensors)
     fn = getattr(_LIB or load(), name)
     if dev == torch.cuda.current_device():
@@ -459,7 +469,9 @@ def exemplar_rmsnorm(x, weight=None, residual=None, eps=1e-6, format=None, strea
     """(y, h, rstd): v = x + residual, h = v in x's type (x itself without a
     residual), y = v * weight / sqrt(mean(v^2) + eps) as a tensor of x's type,
     or as MxRows of ``format``, and rstd = 1 / sqrt(...) in float32 (see
-    exemplar_rmsnorm in exemcl.h)."""
+    exemplar_rmsnorm in exemcl.h).  No autograd graph is recorded, and tensors
+    that require a gradient are refused outside torch.no_grad():
+    exemplar_rmsnorm_backward is the gradient."""
     import torch
     if x.dim() != 2:
         raise ValueError("x must be n x d")
