@@ -405,10 +405,17 @@ hipError_t product_tiled(const MxProductArgs &a, hipStream_t st) {
     return hipGetLastError();
 }
 
-// The kernel for a size.  Where a tile of 64 x 128 leaves most CUs without one,
-// 16 x 16 tiles with the coordinates dealt out to four wavefronts; else the
-// largest tile that still makes enough of them (us, to bf16; 8 and 4: bits of A):
+// The kernel for a size.  16 x 16 tiles, with the coordinates dealt out to four
+// wavefronts, where a fitted time says that they take less than tiles of 64 x 128:
+// mostly up to 16 rows; else the largest tile that still makes enough of them (us,
+// to bf16; 8 and 4: bits of A):
 //                            16x16  64x128  128x128  128x256  256x256
+//   1 x 28 672 x 8 192     8  36.6    65.0
+//                          4  35.3    35.5
+//   8 x 28 672 x 8 192     8  51.9    66.1
+//                          4  45.0    36.3
+//   8 x 20 000 x 1 536     8   8.5    16.5     17.0     23.6
+//                          4   7.1     9.0      9.3     14.5
 //   24 x 2 000 x 1 024     8   3.7    12.1     12.6     17.4
 //                          4   3.4     7.2      7.3     10.6
 //   130 x 8 192 x 1 024    8  23.3    12.6     13.2     18.7     30.0
@@ -433,10 +440,13 @@ hipError_t product_run(const MxProductArgs &a, hipStream_t st) {
     const int64_t cus = std::max<int64_t>(1, device_cu_count());
     auto tiles = [&](int64_t bm, int64_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
     const double ks = (double)(mx_padded(a.d) / kMxRow);
-    // us, fitted to 8 to 4 096 x 300 to 30 000 x 256 to 4 096
-    const double direct = 3.2 + 0.1 * ks + (BITS_A == 8 ? 5e-4 : 4e-4) * (double)tiles(16, 16) * (ks + 0.5);
-    const double tiled = 5.4 + (BITS_A == 8 ? 0.9 : 0.3) * ks;
-    if (direct <= tiled * std::max(1.0, (double)tiles(64, 128) / (2.0 * cus))) return product_direct<T, BITS_A>(a, st);
+    // us, fitted to 1 to 512 x 2 000 to 50 000 x 256 to 8 192.  A tile of 16 x 16
+    // takes half its time for B and half for the rows of A that there are; tiles of
+    // 64 x 128 two to a CU half of what they take one after the other.
+    const double rows = 0.5 * (double)((a.m + 15) / 16) + (double)a.m / 32.0;
+    const double direct = 2.6 + 0.06 * ks + (BITS_A == 8 ? 4.6e-4 : 3.8e-4) * rows * (double)((a.n + 15) / 16) * (ks + 0.5);
+    const double tiled = (5.8 + (BITS_A == 8 ? 0.9 : 0.3) * ks) * (1.0 + (double)std::max<int64_t>(0, tiles(64, 128) - cus) / (2.0 * cus));
+    if (direct <= tiled) return product_direct<T, BITS_A>(a, st);
     if (tiles(64, 128) <= cus) return product_tiled<T, BITS_A, 4, 1, 1, 2, 3>(a, st);
     if (tiles(128, 128) * 2 <= (sizeof(T) == 4 ? 5 : 6) * cus)
         return product_tiled<T, BITS_A, 4, 1, 2, 2, BITS_A == 8 ? 3 : 2>(a, st);

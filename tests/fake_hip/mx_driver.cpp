@@ -73,10 +73,32 @@ static void check_members() {
             }
 }
 
+// Calls read from the standard input, a line each: the kernels that each launches.
+static void print_kernels_of_calls() {
+    char what[16];
+    long long a, b, c, d, e;
+    while (scanf("%15s %lld %lld %lld %lld %lld", what, &a, &b, &c, &d, &e) == 6) {
+        const std::string call = what;
+        void *st = fresh_stream();
+        fake::launches.clear();
+        int rc = -1;
+        if (call == "product")  // m n d format precision
+            rc = exemplar_mx_product(kV, kV, a, (int)d, kV, kV, b, c, nullptr, (int)e, kF, st);
+        if (call == "sets")  // n d l k
+            rc = exemplar_mx_eval(kV, kV, a, b, kI, c, d, kF, st);
+        if (call == "gradient")  // n d precision
+            rc = exemplar_rmsnorm_backward(kV, kV, kV, kF, nullptr, a, b, (int)c, kV, kF, st);
+        expect(rc == EXEMCL_OK, "a call", call);
+        for (const auto &x : fake::launches) printf("%s ", x.name.c_str());
+        printf("\n");
+    }
+}
+
 int main(int argc, char **argv) {
     const std::string what = argc > 1 ? argv[1] : "";
     if (what == "capture") check_capture();
     else if (what == "members") check_members();
+    else if (what == "calls") print_kernels_of_calls();
     else expect(false, "no such check", what);
     if (failures) fprintf(stderr, "%d checks failed\n", failures);
     else printf("%s: checks passed\n", what.c_str());

@@ -1,6 +1,7 @@
 """The host code of the calls on microscaled rows over a HIP runtime that
 launches nothing (tests/fake_hip/mx_driver.cpp), without a GPU."""
 import os
+import re
 import subprocess
 
 import pytest
@@ -39,3 +40,54 @@ def run(driver, *args, stdin=""):
 def test_host_runtime(driver, check):
     r = run(driver, check)
     assert r.returncode == 0 and "checks passed" in r.stdout, r.stdout + r.stderr
+
+
+def kernels(driver, calls):
+    """Per call (name and five numbers) the names of its kernels, with the
+    numbers among their template arguments."""
+    r = run(driver, "calls", stdin="".join(" ".join(map(str, c)) + "\n" for c in calls))
+    lines = r.stdout.splitlines()
+    assert r.returncode == 0 and len(lines) == len(calls) + 1, r.stdout + r.stderr
+    out = []
+    for line in lines[:-1]:
+        found = []
+        for name in line.split():
+            plain = re.search(r"\d((?:mx|rmsnorm|column)_\w+?_kernel)(I(.*?)EEv)?", name)
+            if plain:
+                found.append((plain.group(1), *(int(x) for x in re.findall(r"L[ib](\d+)E", (plain.group(3) or "") + "E"))))
+        out.append(found)
+    return out
+
+
+# m, n, d, format of A, precision (0: fp32, 2: bf16), and whether 16 x 16 tiles
+# take less time than 64 x 128 (us of both): the two differ by a tenth or more.
+FEW_ROWS = [
+    (1, 2000, 1024, 8, 2, True),     # 3.1, 11.0
+    (1, 20_000, 1536, 4, 0, True),   # 6.1, 8.4
+    (1, 20_000, 1536, 4, 2, True),   # 6.1, 8.1
+    (1, 20_000, 1536, 8, 2, True),   # 6.8, 15.5
+    (1, 28_672, 8192, 8, 0, True),   # 36.6, 64.5
+    (1, 28_672, 8192, 8, 2, True),   # 36.6, 65.0
+    (1, 50_000, 256, 8, 0, True),    # 5.1, 7.9
+    (1, 50_000, 256, 4, 0, True),    # 4.7, 5.8
+    (4, 28_672, 8192, 8, 2, True),   # 44.3, 65.8
+    (8, 20_000, 1536, 4, 2, True),   # 7.1, 9.0
+    (8, 28_672, 8192, 8, 2, True),   # 51.9, 66.1
+    (16, 20_000, 1536, 4, 0, True),  # 8.4, 10.2
+    (16, 50_000, 256, 8, 2, True),   # 6.7, 8.9
+    (16, 28_672, 8192, 4, 2, False),  # 55.2, 36.6
+    (24, 8192, 4096, 8, 2, True),    # 18.7, 34.0
+    (24, 20_000, 1536, 4, 2, False),  # 12.3, 9.0
+    (24, 28_672, 8192, 8, 2, False),  # 115, 66.4
+    (48, 8192, 1024, 8, 2, True),    # 9.9, 12.3
+    (48, 8192, 4096, 4, 2, False),   # 24.1, 14.8
+    (48, 20_000, 1536, 8, 2, False),  # 23.3, 16.6
+    (130, 8192, 1024, 8, 2, False),  # 23.3, 12.6
+    (130, 8192, 1024, 4, 0, False),  # 19.6, 9.1
+]
+
+
+def test_products_of_few_rows_take_the_faster_kernel(driver):
+    got = kernels(driver, [("product", *c[:5]) for c in FEW_ROWS])
+    for c, (kernel,) in zip(FEW_ROWS, got):
+        assert (kernel[0] == "mx_product_direct_kernel") == c[5], (c, kernel)
