@@ -73,7 +73,8 @@ static void check_members() {
             }
 }
 
-// Calls read from the standard input, a line each: the kernels that each launches.
+// Calls read from the standard input, a line each: the kernels that each launches,
+// with their workgroups.
 static void print_kernels_of_calls() {
     char what[16];
     long long a, b, c, d, e;
@@ -89,9 +90,14 @@ static void print_kernels_of_calls() {
         if (call == "gradient")  // n d precision
             rc = exemplar_rmsnorm_backward(kV, kV, kV, kF, nullptr, a, b, (int)c, kV, kF, st);
         expect(rc == EXEMCL_OK, "a call", call);
-        for (const auto &x : fake::launches) printf("%s ", x.name.c_str());
+        for (const auto &x : fake::launches) printf("%s:%u ", x.name.c_str(), x.grid.x * x.grid.y);
         printf("\n");
     }
+}
+
+// Every kernel in the library.
+static void print_all_kernels() {
+    for (const auto &x : fake::kernels()) printf("%s\n", x.second.c_str());
 }
 
 int main(int argc, char **argv) {
@@ -99,6 +105,7 @@ int main(int argc, char **argv) {
     if (what == "capture") check_capture();
     else if (what == "members") check_members();
     else if (what == "calls") print_kernels_of_calls();
+    else if (what == "all") print_all_kernels();
     else expect(false, "no such check", what);
     if (failures) fprintf(stderr, "%d checks failed\n", failures);
     else printf("%s: checks passed\n", what.c_str());

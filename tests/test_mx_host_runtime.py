@@ -6,6 +6,8 @@ import subprocess
 
 import pytest
 
+import mx_sizes
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
@@ -43,20 +45,28 @@ def test_host_runtime(driver, check):
 
 
 def kernels(driver, calls):
-    """Per call (name and five numbers) the names of its kernels, with the
-    numbers among their template arguments."""
-    r = run(driver, "calls", stdin="".join(" ".join(map(str, c)) + "\n" for c in calls))
+    """Per call (name and up to five numbers) its kernels, as plain_name has them."""
+    r = run(driver, "calls", stdin="".join(" ".join(map(str, (*c, 0, 0, 0)[:6])) + "\n" for c in calls))
     lines = r.stdout.splitlines()
     assert r.returncode == 0 and len(lines) == len(calls) + 1, r.stdout + r.stderr
-    out = []
-    for line in lines[:-1]:
-        found = []
-        for name in line.split():
-            plain = re.search(r"\d((?:mx|rmsnorm|column)_\w+?_kernel)(I(.*?)EEv)?", name)
-            if plain:
-                found.append((plain.group(1), *(int(x) for x in re.findall(r"L[ib](\d+)E", (plain.group(3) or "") + "E"))))
-        out.append(found)
-    return out
+    return [[k for k in map(plain_name, line.split()) if k] for line in lines[:-1]]
+
+
+def plain_name(symbol):
+    """(name, element type, numbers) of a kernel on rows from "symbol:workgroups"."""
+    m = re.search(r"\d((?:mx|rmsnorm|column)_[a-z0-9_]+?_kernel)(I(.*?)EEv)?", symbol)
+    if not m:
+        return None
+    args = m.group(3) or ""
+    kind = re.match(r"DF16b|DF16_|f", args)
+    return (m.group(1), kind.group(0) if kind else "", *(int(x) for x in re.findall(r"L[ib](\d+)E", args + "E")))
+
+
+def compiled(driver, name):
+    """Every kernel of the library whose name starts so."""
+    r = run(driver, "all")
+    assert r.returncode == 0
+    return {k for k in map(plain_name, r.stdout.split()) if k and k[0].startswith(name)}
 
 
 # m, n, d, format of A, precision (0: fp32, 2: bf16), and whether 16 x 16 tiles
@@ -91,3 +101,10 @@ def test_products_of_few_rows_take_the_faster_kernel(driver):
     got = kernels(driver, [("product", *c[:5]) for c in FEW_ROWS])
     for c, (kernel,) in zip(FEW_ROWS, got):
         assert (kernel[0] == "mx_product_direct_kernel") == c[5], (c, kernel)
+
+
+def test_sizes_of_products_take_every_kernel(driver):
+    """A kernel that is compiled is run by the tests on the GPU, whatever the rule
+    that chooses it."""
+    calls = [("product", *size, fmt, prec) for size in mx_sizes.PRODUCTS for fmt in (4, 8) for prec in (0, 1, 2)]
+    assert {k for found in kernels(driver, calls) for k in found} == compiled(driver, "mx_product")
