@@ -4,3 +4,13 @@
 # Products (m, n, d): few results, then tiles of 64 x 128, 128 x 128, 128 x 256 and,
 # with A of 4 bits, 256 x 256; nothing is a whole number of tiles or steps.
 PRODUCTS = [(1, 333, 700), (19, 1001, 260), (130, 8191, 500), (300, 9000, 700), (1031, 12_001, 400), (1030, 12_101, 1500)]
+
+# Sets (n, d, l, k).  Rows of every number of 128 coordinates that has kernels of
+# its own, and of one less where two share them.  Of each: many points, several set
+# groups to a workgroup, an odd number of members, the last group not full; few
+# points and groups; one block of points and very many groups.
+SETS_D = [100, 250, 383, 500, 620, 700, 800, 1000, 1100, 1250, 1400, 1500, 1650, 1700, 1900, 2000]
+SETS = [(n, d, l, k) for d in SETS_D for n, l, k in ((40_011, 300, 7), (3001, 100, 19), (100, 30_001, 3))]
+# Rows short enough for workgroups that stage their sets themselves, and too long
+# for all the others.
+SETS += [(10_000, 60, 45, 8), (4001, 200, 45, 5), (3001, 2176, 100, 5), (130, 4100, 300, 9)]

@@ -46,10 +46,14 @@ def test_host_runtime(driver, check):
 
 def kernels(driver, calls):
     """Per call (name and up to five numbers) its kernels, as plain_name has them."""
+    return [[k for k in map(plain_name, line.split()) if k] for line in run_calls(driver, calls)]
+
+
+def run_calls(driver, calls):
     r = run(driver, "calls", stdin="".join(" ".join(map(str, (*c, 0, 0, 0)[:6])) + "\n" for c in calls))
     lines = r.stdout.splitlines()
     assert r.returncode == 0 and len(lines) == len(calls) + 1, r.stdout + r.stderr
-    return [[k for k in map(plain_name, line.split()) if k] for line in lines[:-1]]
+    return lines[:-1]
 
 
 def plain_name(symbol):
@@ -108,3 +112,21 @@ def test_sizes_of_products_take_every_kernel(driver):
     that chooses it."""
     calls = [("product", *size, fmt, prec) for size in mx_sizes.PRODUCTS for fmt in (4, 8) for prec in (0, 1, 2)]
     assert {k for found in kernels(driver, calls) for k in found} == compiled(driver, "mx_product")
+
+
+def test_sizes_of_sets_take_every_kernel(driver):
+    """As with products; and the batch kernels take several groups of 16 sets one
+    after the other in a workgroup."""
+    calls = [("sets", *size) for size in mx_sizes.SETS]
+    found = kernels(driver, calls)
+    # (few points do not fill mx_fold_kernel's rows: test_sets_on_many_points)
+    assert {k for f in found for k in f} | {("mx_fold_kernel", "")} == compiled(driver, ("mx_sets", "mx_bias", "mx_fold"))
+    several = set()
+    for (n, d, l, k), line in zip(mx_sizes.SETS, run_calls(driver, calls)):
+        for symbol in line.split():
+            name = plain_name(symbol)
+            if name and name[0] == "mx_sets_kernel":
+                points, groups = name[3] * name[4] * 16, -(-l // 16)
+                if int(symbol.split(":")[1]) < -(-n // points) * groups:
+                    several.add(name)
+    assert {k[2:5] for k in several} == {k[2:5] for k in compiled(driver, "mx_sets_kernel")}
