@@ -14,3 +14,8 @@ SETS = [(n, d, l, k) for d in SETS_D for n, l, k in ((40_011, 300, 7), (3001, 10
 # Rows short enough for workgroups that stage their sets themselves, and too long
 # for all the others.
 SETS += [(10_000, 60, 45, 8), (4001, 200, 45, 5), (3001, 2176, 100, 5), (130, 4100, 300, 9)]
+
+# Gradients of the norm (n, d), each kernel with so many rows that a thread takes
+# several of them after each other: 512 workgroups of 16, 4 or 1 rows at a time.
+GRADIENTS = [(17_003, 100), (8300, 256), (2100, 500), (4150, 1000), (2500, 1303), (2051, 2048), (1300, 2049), (1037, 4096),
+             (1025, 5003), (530, 8192), (70, 8200)]

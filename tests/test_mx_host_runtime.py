@@ -130,3 +130,14 @@ def test_sizes_of_sets_take_every_kernel(driver):
                 if int(symbol.split(":")[1]) < -(-n // points) * groups:
                     several.add(name)
     assert {k[2:5] for k in several} == {k[2:5] for k in compiled(driver, "mx_sets_kernel")}
+
+
+def test_sizes_of_gradients_take_every_kernel(driver):
+    calls = [("gradient", *size, prec) for size in mx_sizes.GRADIENTS for prec in (0, 1, 2)]
+    every = compiled(driver, ("rmsnorm_grad", "rmsnorm_dw", "column_sum"))
+    assert {k for found in kernels(driver, calls) for k in found} == every
+    for (n, d), line in zip(mx_sizes.GRADIENTS, run_calls(driver, calls)[::3]):
+        for symbol in line.split():
+            kind = plain_name(symbol)
+            if kind and kind[0] == "rmsnorm_grad_kernel":  # more rows than workgroups take at once
+                assert n > int(symbol.split(":")[1]) * (256 // kind[2]), (n, d, symbol)

@@ -1,9 +1,11 @@
-"""The norm to microscaled rows where a row's root, or a result, is not finite."""
+"""The norm to microscaled rows where a row's root, or a result, is not finite; its
+gradient over many rows; rounding of more rows than one launch takes."""
 import numpy as np
 import pytest
 import torch
 
 import mx_reference as ref
+import mx_sizes
 from paper_2101_08763_amd import api
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +50,52 @@ def test_results_past_the_range_of_fp32(fmt):
     c, s = ref.quantize(want, fmt)
     assert np.array_equal(scales[1], s[0])
     assert np.array_equal(ref.values(codes[1:2], scales[1:2], 64, fmt), ref.values(c, s, 64, fmt))
+
+
+UNIT = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}  # half a step, relative
+TINY = {torch.float32: 2.0 ** -149, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}
+
+
+@pytest.mark.parametrize("weight,stream", [(True, True), (False, False)])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n,d", mx_sizes.GRADIENTS)
+def test_gradient_over_many_rows(n, d, dtype, weight, stream):
+    """dx: 32 additions a thread, 8 in its wavefront and workgroup and a few
+    products, 60 roundings of 2^-24 of the terms' magnitudes.  dweight: a thread
+    adds n / 512 rows or fewer than n / 64 (d > 8 192), 16 threads' sums follow in
+    32 bits, the rest in 64; each term has two roundings."""
+    g = torch.Generator("cuda").manual_seed(n + d)
+    h, dy, dh = ((a * torch.randn(n, d, generator=g, device="cuda")).to(dtype) for a in (1.5, 1.0, 1.0))
+    w = (1 + 0.2 * torch.randn(d, generator=g, device="cuda")).to(dtype) if weight else None
+    rstd = torch.rsqrt(h.float().square().mean(1) + 1e-5)
+    dx, dw = api.exemplar_rmsnorm_backward(dy, h, w, rstd, dh=dh if stream else None)
+    s = rstd.double()[:, None]
+    xhat, out = h.double() * s, dy.double()
+    grad = out * w.double() if weight else out
+    want = s * (grad - xhat * (grad * xhat).mean(1, keepdim=True)) + (dh.double() if stream else 0.0)
+    size = s * (grad.abs() + xhat.abs() * (grad * xhat).abs().mean(1, keepdim=True)) + (dh.double().abs() if stream else 0.0)
+    assert torch.all((dx.double() - want).abs() <= 60 * 2.0 ** -24 * size + UNIT[dtype] * 1.001 * want.abs() + TINY[dtype])
+    terms = out * xhat
+    bound = (n / 64 + 20) * 2.0 ** -24 * terms.abs().sum(0)
+    assert torch.all((dw.double() - terms.sum(0)).abs() <= bound)
+
+
+def test_rounding_in_several_launches():
+    """2^26 rows of 16 chunks and a few more: the second launch starts where the
+    first one ended, there and back."""
+    n, d = (1 << 26) + 37, 128
+    x = torch.empty(n, d, dtype=torch.float16, device="cuda")
+    x[:1 << 20].normal_(generator=torch.Generator("cuda").manual_seed(5))
+    for i in range(1 << 20, n, 1 << 20):  # the same, shifted by a coordinate a block of rows
+        m = min(1 << 20, n - i)
+        x[i:i + m] = x[:m].roll(i >> 20, 1)
+    q = api.exemplar_mx_quantize(x, FP4)
+    near = torch.cat([torch.arange(5), torch.arange(-40, 37) + (1 << 26), torch.arange(7) + (1 << 25)])
+    codes, scales = ref.quantize(x[near.cuda()].cpu().double().numpy(), FP4)
+    assert np.array_equal(q.scales[near.cuda()].cpu().numpy(), scales)
+    got = q.codes[near.cuda()].cpu().numpy()
+    assert np.array_equal(ref.values(got, scales, d, FP4), ref.values(codes, scales, d, FP4))
+    del x
+    back = api.exemplar_mx_dequantize(q, torch.float16)
+    want = torch.as_tensor(ref.values(codes, scales, d, FP4)).half()
+    assert torch.equal(back[near.cuda()].cpu(), want)
