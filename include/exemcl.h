@@ -336,7 +336,7 @@ EXEMCL_API int exemplar_mx_quantize(const void *x, int64_t n, int64_t d, int pre
 /*
  * exemplar_mx_dequantize -- the values of n rows, as n x d elements of type
  * `precision` (exact in fp32 and bf16 down to their subnormal numbers; fp16
- * rounds, and what is past its range becomes infinite).
+ * rounds; what is past a type's range becomes infinite).
  */
 EXEMCL_API int exemplar_mx_dequantize(const void *codes, const void *scales, int64_t n, int64_t d, int format,
                                       int precision, void *x, void *stream);
@@ -345,8 +345,9 @@ EXEMCL_API int exemplar_mx_dequantize(const void *codes, const void *scales, int
  * exemplar_rmsnorm -- root-mean-square norm of n rows, with the residual's
  * addition before it and the rounding to microscaled rows behind it:
  *   v = x + residual,  y = v * weight / sqrt(mean(v^2) + eps).
- * v is in fp32 and not rounded again, the mean and its root are in fp64.  A y past
- * fp32's range is infinite (and its block NaN).
+ * v is in fp32 and not rounded again, the mean and its root are in fp64, rstd is
+ * their result in fp32.  An rstd past its range (eps = 0 and a root mean square
+ * below 2^-128) or a y is infinite, and a block with such a y NaN.
  *
  *   x, residual  device, n x d row-major, type per `precision`; residual may be
  *                NULL (v = x)
@@ -379,7 +380,7 @@ EXEMCL_API int exemplar_rmsnorm(const void *x, const void *residual, const void 
  *   dweight  device, d floats; written (zeros where n = 0); may be NULL
  *
  * Sums over the rows are taken in a fixed order, so the result is bitwise
- * reproducible.  Temporary memory: up to 1 024 x d floats.
+ * reproducible.  Temporary memory: up to 512 x d floats.
  */
 EXEMCL_API int exemplar_rmsnorm_backward(const void *dy, const void *h, const void *weight, const float *rstd,
                                          const void *dh, int64_t n, int64_t d, int precision, void *dx, float *dweight,
@@ -397,7 +398,7 @@ EXEMCL_API int exemplar_rmsnorm_backward(const void *dy, const void *h, const vo
  *
  * Sums are those of fp32, whatever the type of C: the products of 8
  * consecutive coordinates are added exactly (of 8-bit rows in two parts), the
- * rest with fp32's rounding, and C's type rounds once.  A NaN block makes its row's or column's results NaN.
+ * rest in fp32, and C's type rounds once.  A NaN block makes its row's or column's results NaN.
  */
 EXEMCL_API int exemplar_mx_product(const void *A, const void *A_scales, int64_t m, int format_a, const void *B,
                                    const void *B_scales, int64_t n, int64_t d, const float *bias, int precision, void *C,

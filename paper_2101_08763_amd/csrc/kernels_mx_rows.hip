@@ -27,7 +27,7 @@ constexpr int64_t kMaxChunks = int64_t(1) << 30;
 
 // ---------------------------------------------------------------------------
 // Rounding.  A lane takes 8 coordinates, four lanes a block.  HBM-bound: 10^6 x
-// 256 fp16 to 4 bits in 115 us (5.7 TB/s) and back in 88 (7.4).
+// 256 fp16 to 4 bits in 112 us (5.8 TB/s) and back in 93 (7.0).
 // ---------------------------------------------------------------------------
 template <typename T, int BITS>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T *__restrict__ x, uint32_t chunks, Divider per_row,
@@ -379,7 +379,7 @@ hipError_t quantize(const void *x, int64_t n, int64_t d, void *codes, void *scal
 }
 
 // Values that do not fit the last-level cache (256 MiB) are stored past it: 512
-// MB of fp16 in 88 us instead of 126.  Smaller ones may be read from it next.
+// MB of fp16 in 93 us instead of 126.  Smaller ones may be read from it next.
 constexpr int64_t kStreamBytes = int64_t(256) << 20;
 
 template <typename T, int BITS>

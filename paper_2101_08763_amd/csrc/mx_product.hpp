@@ -72,11 +72,12 @@ __global__ __launch_bounds__(kDirectWaves * 64) void mx_product_direct_kernel(
 // own order, takes the address units 64 steps a load instead of 16: 16 384 x
 // 8 192 x 4 096 565 us).
 //
-// That size, 8 by 4 bits to bf16, takes 654 us: two instructions for every 128
-// coordinates (mx_divide), together at 3.4 PFLOP/s where the instruction alone, on
-// random values, runs at 4.2.  4 by 4 bits takes 312 (3.5 of 6.8).  The rest is the
-// start and the end of a tile, LDS reads and copies between instructions, and the
-// clock, which the chip lowers on random values.
+// That size, 8 by 4 bits to bf16, takes 662 us: two instructions for every 128
+// coordinates (mx_divide), together at 3.3 PFLOP/s where the instruction alone, on
+// random values, runs at 4.2; the matrix cores are busy 75 % of the time.  4 by 4
+// bits takes 312 (3.5 of 6.8).  The rest is the start and the end of a tile, LDS
+// reads and copies between instructions, and the clock, which the chip lowers on
+// random values.
 // ---------------------------------------------------------------------------
 template <int BITS_A, int WM, int NB, int PM, int PN, int DEPTH>
 struct MxTilePlan {
@@ -88,7 +89,8 @@ struct MxTilePlan {
     // 16-byte chunks of a row in a stage, 4 or 8 (4- or 8-bit rows); chunk c of
     // row p goes to place c ^ swap(p).  The 16 rows that lanes read the same
     // chunk of then fill all 64 banks once, and so do 8 such rows and the 8
-    // others of the next chunk.
+    // others of the next chunk.  (The conflicts that are counted, two cycles for
+    // each, are those of the scales' byte reads.)
     static constexpr int A_CHUNKS = BITS_A;
     template <int CHUNKS>
     __device__ __forceinline__ static int swap(int p) {
