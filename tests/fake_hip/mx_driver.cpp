@@ -89,6 +89,12 @@ static void print_kernels_of_calls() {
             rc = exemplar_mx_eval(kV, kV, a, b, kI, c, d, kF, st);
         if (call == "gradient")  // n d precision
             rc = exemplar_rmsnorm_backward(kV, kV, kV, kF, nullptr, a, b, (int)c, kV, kF, st);
+        if (call == "norm")  // n d precision format
+            rc = exemplar_rmsnorm(kV, kV, kV, a, b, (int)c, 1e-6f, (int)d, kV, kV, kV, kF, st);
+        if (call == "quantize")  // n d precision format
+            rc = exemplar_mx_quantize(kV, a, b, (int)c, (int)d, kV, kV, st);
+        if (call == "dequantize")  // n d precision format
+            rc = exemplar_mx_dequantize(kV, kV, a, b, (int)d, (int)c, kV, st);
         expect(rc == EXEMCL_OK, "a call", call);
         for (const auto &x : fake::launches) printf("%s:%u ", x.name.c_str(), x.grid.x * x.grid.y);
         printf("\n");

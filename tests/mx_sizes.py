@@ -19,3 +19,7 @@ SETS += [(10_000, 60, 45, 8), (4001, 200, 45, 5), (3001, 2176, 100, 5), (130, 41
 # several of them after each other: 512 workgroups of 16, 4 or 1 rows at a time.
 GRADIENTS = [(17_003, 100), (8300, 256), (2100, 500), (4150, 1000), (2500, 1303), (2051, 2048), (1300, 2049), (1037, 4096),
              (1025, 5003), (530, 8192), (70, 8200)]
+
+# Rounding there and back (n, d): results that fit the last-level cache, and more
+# than 256 MiB of them in every type.
+ROUNDINGS = [(65, 100), (300_007, 499)]

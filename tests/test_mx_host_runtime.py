@@ -141,3 +141,13 @@ def test_sizes_of_gradients_take_every_kernel(driver):
             kind = plain_name(symbol)
             if kind and kind[0] == "rmsnorm_grad_kernel":  # more rows than workgroups take at once
                 assert n > int(symbol.split(":")[1]) * (256 // kind[2]), (n, d, symbol)
+
+
+def test_sizes_of_norms_and_roundings_take_every_kernel(driver):
+    from test_mx_gpu import NORM_SIZES
+    norms = [("norm", n, d, prec, fmt) for n, d in NORM_SIZES for prec in (0, 1, 2) for fmt in (0, 4, 8)]
+    assert {k for found in kernels(driver, norms) for k in found} == compiled(driver, "rmsnorm_kernel")
+    there_and_back = [(way, n, d, prec, fmt) for way in ("quantize", "dequantize") for n, d in mx_sizes.ROUNDINGS
+                      for prec in (0, 1, 2) for fmt in (4, 8)]
+    every = compiled(driver, ("mx_quantize", "mx_dequantize"))
+    assert {k for found in kernels(driver, there_and_back) for k in found} == every

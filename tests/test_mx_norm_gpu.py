@@ -80,6 +80,27 @@ def test_gradient_over_many_rows(n, d, dtype, weight, stream):
     assert torch.all((dw.double() - terms.sum(0)).abs() <= bound)
 
 
+@pytest.mark.parametrize("fmt", [FP4, FP8])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n,d", mx_sizes.ROUNDINGS)
+def test_rounding_there_and_back(n, d, dtype, fmt):
+    """Every element: rounding what rows stand for gives these rows again, and its
+    values do not depend on how many rows there are."""
+    g = torch.Generator("cuda").manual_seed(n + fmt)
+    x = torch.randn(n, d, generator=g, device="cuda").to(dtype)
+    q = api.exemplar_mx_quantize(x, fmt)
+    back = api.exemplar_mx_dequantize(q, dtype)
+    again = api.exemplar_mx_quantize(back, fmt)
+    assert torch.equal(again.scales, q.scales)
+    assert torch.equal(api.exemplar_mx_dequantize(again, dtype), back)
+    for i in range(0, n, 50_000):
+        part = api.MxRows(q.codes[i:i + 50_000], q.scales[i:i + 50_000], d, fmt)
+        assert torch.equal(api.exemplar_mx_dequantize(part, dtype), back[i:i + 50_000])
+    near = [0, 1, n // 3, n - 2, n - 1]
+    codes, scales = ref.quantize(x[near].cpu().double().numpy(), fmt)
+    assert np.array_equal(back[near].cpu().double().numpy(), ref.values(codes, scales, d, fmt))
+
+
 def test_rounding_in_several_launches():
     """2^26 rows of 16 chunks and a few more: the second launch starts where the
     first one ended, there and back."""
