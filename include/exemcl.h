@@ -413,6 +413,133 @@ EXEMCL_API int exemplar_mx_product(const void *A, const void *A_scales, int64_t 
 EXEMCL_API int exemplar_mx_eval(const void *codes, const void *scales, int64_t n, int64_t d, const int32_t *sets,
                                 int64_t l, int64_t k, float *out, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Gated feed-forward block: what a model has between the norm of a residual
+ * stream and the projection that makes embeddings of it.  With rows x (n x d) and
+ * two weights (f x d, a row for every result),
+ *   g = x Wg' + bg,  u = x Wu' + bu,  h = a(g) * u   (n x f, element by element)
+ * for one of the activations below.  exemplar_glu and exemplar_glu_backward are for
+ * weights of the rows' type (training); exemplar_w4_glu has them in 4 bits with
+ * group scales (serving), and exemplar_w4_product is the product by one such
+ * weight, which is also what follows the block.
+ *
+ * The conventions above (ownership, streams, asynchrony, dense row-major arrays)
+ * hold, n and f may be 0 (nothing is queued where nothing is written, and the arrays
+ * may be NULL), and infinities and NaN go the way of arithmetic (of fp32 rows and
+ * weights in exemplar_glu and its gradient an infinity may come out as NaN).  Outputs
+ * must not overlap inputs.  All sums are in fp32 or wider, in an order that the
+ * sizes decide: results are bitwise reproducible.
+ *
+ * Temporary memory, taken as exemplar_eval does: exemplar_glu_backward always (n > 0,
+ * f > 0) and exemplar_glu of more than 64 rows where x, Wg or Wu has to be laid out
+ * again (fp32, d not a multiple of 8, an address not a multiple of 16 bytes).  On a
+ * capturing stream those calls return EINVAL and queue nothing; the others may be
+ * captured.
+ * ------------------------------------------------------------------------ */
+enum exemcl_activation {
+    EXEMCL_SILU = 0,      /* g / (1 + e^-g) */
+    EXEMCL_GELU = 1,      /* g Phi(g), Phi the normal distribution */
+    EXEMCL_GELU_TANH = 2, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+    EXEMCL_RELU = 3       /* max(g, 0), with the derivative 0 at 0 */
+};
+
+/*
+ * exemplar_glu -- h = a(x Wg' + bg) * (x Wu' + bu).
+ *
+ *   x          device, n x d, type per `precision`; 1 <= d <= 2^20
+ *   Wg, Wu     device, f x d of the same type; 0 <= f <= 2^20
+ *   bg, bu     device, f floats each; NULL: 0
+ *   activation one of exemcl_activation
+ *   h          device, n x f of the same type; written
+ *   g, u       device, n x f of the same type: what exemplar_glu_backward needs,
+ *              rounded; either may be NULL (h is made from the unrounded values)
+ *
+ * Each result is rounded once.  fp32 products are those of three bf16 parts of each
+ * value, six products for one, which leave out less than 2^-26 of it.
+ */
+EXEMCL_API int exemplar_glu(const void *x, int64_t n, int64_t d, const void *Wg, const void *Wu, int64_t f,
+                            const float *bg, const float *bu, int precision, int activation, void *h, void *g, void *u,
+                            void *stream);
+
+/*
+ * exemplar_glu_backward -- the gradient of exemplar_glu from dh, that of h: with
+ * dg = dh * u * a'(g) and du = dh * a(g),
+ *   dx = dg Wg + du Wu,  dWg = dg' x,  dWu = du' x,  dbg = sum_rows dg,  dbu = sum_rows du.
+ *
+ *   dh, g, u   device, n x f, type per `precision`; g and u as exemplar_glu wrote them
+ *   x, Wg, Wu  as given to exemplar_glu (x may be NULL without dWg and dWu, the weights
+ *              without dx)
+ *   dx         device, n x d of the type; dWg, dWu: f x d of the type; dbg, dbu: f
+ *              floats.  Written; each may be NULL and is then not computed.  For
+ *              n = 0 the sums are zeros.
+ *
+ * The products take dg and du rounded to the type (fp32: in three bf16 parts); the
+ * sums dbg and dbu take them unrounded.  dx is one sum over both matrices.
+ * Temporary memory: dg and du (4 n f bytes; fp32: 12 n f), up to 4096 f bytes for the
+ * sums, and x, Wg and Wu where they have to be laid out again.
+ */
+EXEMCL_API int exemplar_glu_backward(const void *dh, const void *x, const void *Wg, const void *Wu, const void *g,
+                                     const void *u, int64_t n, int64_t d, int64_t f, int precision, int activation,
+                                     void *dx, void *dWg, void *dWu, float *dbg, float *dbu, void *stream);
+
+/*
+ * Weights of 4 bits with group scales: n rows of d coordinates (1 <= d <= 2^22), each
+ * q = 0 .. 15 standing for (q - z) * s with a scale s and a zero point z for every
+ * `group` = 32, 64 or 128 consecutive coordinates of a row.  Two dense arrays, both
+ * 16-byte aligned, in the order in which the matrix cores take them; np is n rounded
+ * up to a multiple of 16 and dp is d rounded up to one of 128:
+ *   codes   np x dp / 2 bytes, tiles of 16 rows x 128 coordinates (1 KiB): tile
+ *           (i, b) = rows 16 i .. 16 i + 15, coordinates 128 b .. 128 b + 127 at
+ *           1024 (i dp/128 + b).  In it, row r's coordinate 32 j + 8 p + e (e < 8)
+ *           is in byte 256 p + 16 r + 4 j + e % 4: e < 4 its low half, else its high.
+ *   words   np x dp / group 32-bit words, 16 rows together: group c of row
+ *           16 i + r at (i dp/group + c) 16 + r.  A word is z (0 .. 255) in its last 8
+ *           bits and an fp32 number in the others, s with 16 significant bits: any
+ *           fp16 or bf16 number is one.
+ * Rows past n have any codes and words; a group's coordinates past d any codes.
+ */
+
+/*
+ * exemplar_w4_layout -- bytes of codes and number of words of n rows of d
+ * coordinates (either pointer may be NULL); host only.  EINVAL for n < 0,
+ * n > INT32_MAX, d < 1, d > 2^22 or another group.
+ */
+EXEMCL_API int exemplar_w4_layout(int64_t n, int64_t d, int group, int64_t *code_bytes, int64_t *words);
+
+/*
+ * exemplar_w4_quantize -- rounds n rows of d coordinates.  With lo and hi the least
+ * and largest value of a group and of 0, s = (hi - lo) / 15 rounded up to 16
+ * significant bits (0 below 2^-126: the group counts as zeros), and with r the fp32
+ * reciprocal of s, z = round(-lo r) and q = round(v r) + z, both within 0 .. 15,
+ * ties to even.  A group that holds an infinity or a NaN is all NaN.
+ *
+ *   w             device, n x d row-major, type per `precision`
+ *   codes, words  device; written, padding included
+ */
+EXEMCL_API int exemplar_w4_quantize(const void *w, int64_t n, int64_t d, int precision, int group, void *codes,
+                                    uint32_t *words, void *stream);
+
+/* exemplar_w4_dequantize -- the values of n rows, as n x d elements of type `precision`. */
+EXEMCL_API int exemplar_w4_dequantize(const void *codes, const uint32_t *words, int64_t n, int64_t d, int group,
+                                      int precision, void *w, void *stream);
+
+/*
+ * exemplar_w4_product -- y = x W' + bias for rows x (n x d, type per `precision`, not
+ * rounded further) and weights of f rows of 4 bits; y is n x f of x's type, bias f
+ * floats or NULL.  A group's products are added with whole q, and s and z applied to
+ * the sum, in fp32.  No temporary memory.
+ */
+EXEMCL_API int exemplar_w4_product(const void *x, int64_t n, int64_t d, int precision, const void *codes,
+                                   const uint32_t *words, int64_t f, int group, const float *bias, void *y, void *stream);
+
+/*
+ * exemplar_w4_glu -- exemplar_glu on two weights of 4 bits with groups of the same
+ * size; h as there.  No temporary memory.
+ */
+EXEMCL_API int exemplar_w4_glu(const void *x, int64_t n, int64_t d, int precision, const void *gate_codes,
+                               const uint32_t *gate_words, const void *up_codes, const uint32_t *up_words, int64_t f,
+                               int group, const float *bg, const float *bu, int activation, void *h, void *stream);
+
 /*
  * exemplar_plan -- host-only description of what exemplar_eval would launch
  * for these sizes; touches no device.  Writes the chosen exemcl_path to

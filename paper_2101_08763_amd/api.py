@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(PKG, "libexemcl.so")
 
 EXEMCL_FP32, EXEMCL_FP16, EXEMCL_BF16 = 0, 1, 2
 EXEMCL_MX_NONE, EXEMCL_MXFP4, EXEMCL_MXFP8 = 0, 4, 8
+EXEMCL_SILU, EXEMCL_GELU, EXEMCL_GELU_TANH, EXEMCL_RELU = 0, 1, 2, 3
 EXEMCL_OK, EXEMCL_EINVAL, EXEMCL_ENOMEM, EXEMCL_EDEVICE, EXEMCL_ESCRATCH = 0, 1, 2, 3, 4
 EXEMCL_SCRATCH_BYTES = 64 << 20   # fixed scratch buffer of exemplar_eval_noalloc
 PATH_NONE, PATH_VALU, PATH_MFMA = 0, 1, 2
@@ -26,6 +27,8 @@ PATH_NAMES = {PATH_NONE: "none", PATH_VALU: "valu", PATH_MFMA: "mfma"}
 EXPORTED = ("exemplar_eval", "exemplar_eval_noalloc", "exemplar_eval_streamed", "exemplar_gain", "exemplar_greedy", "exemplar_sqnorm",
             "exemplar_plan", "exemplar_mx_layout", "exemplar_mx_quantize", "exemplar_mx_dequantize", "exemplar_rmsnorm",
             "exemplar_rmsnorm_backward", "exemplar_mx_product", "exemplar_mx_eval",
+            "exemplar_glu", "exemplar_glu_backward", "exemplar_w4_layout", "exemplar_w4_quantize", "exemplar_w4_dequantize",
+            "exemplar_w4_product", "exemplar_w4_glu",
             "exemplar_prof_enable", "exemplar_prof_read", "exemplar_strerror", "exemplar_version")
 
 
@@ -80,6 +83,20 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.exemplar_mx_product.restype = ip
     lib.exemplar_mx_eval.argtypes = [vp, vp, i64, i64, vp, i64, i64, vp, vp]
     lib.exemplar_mx_eval.restype = ip
+    lib.exemplar_glu.argtypes = [vp, i64, i64, vp, vp, i64, vp, vp, ip, ip, vp, vp, vp, vp]
+    lib.exemplar_glu.restype = ip
+    lib.exemplar_glu_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ip, ip, vp, vp, vp, vp, vp, vp]
+    lib.exemplar_glu_backward.restype = ip
+    lib.exemplar_w4_layout.argtypes = [i64, i64, ip, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)]
+    lib.exemplar_w4_layout.restype = ip
+    lib.exemplar_w4_quantize.argtypes = [vp, i64, i64, ip, ip, vp, vp, vp]
+    lib.exemplar_w4_quantize.restype = ip
+    lib.exemplar_w4_dequantize.argtypes = [vp, vp, i64, i64, ip, ip, vp, vp]
+    lib.exemplar_w4_dequantize.restype = ip
+    lib.exemplar_w4_product.argtypes = [vp, i64, i64, ip, vp, vp, i64, ip, vp, vp, vp]
+    lib.exemplar_w4_product.restype = ip
+    lib.exemplar_w4_glu.argtypes = [vp, i64, i64, ip, vp, vp, vp, vp, i64, ip, vp, vp, ip, vp, vp]
+    lib.exemplar_w4_glu.restype = ip
     lib.exemplar_strerror.argtypes = [ip]
     lib.exemplar_strerror.restype = ctypes.c_char_p
     lib.exemplar_prof_enable.argtypes = [ip]
@@ -391,9 +408,10 @@ def _check_gradient(name, tensors):
     """Results carry no autograd graph: a gradient that is asked for would be lost
     without a word.  (Codes of rows have none to lose.)"""
     import torch
-    if name != "exemplar_mx_quantize" and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+    if name not in ("exemplar_mx_quantize", "exemplar_w4_quantize") and torch.is_grad_enabled() \
+            and any(t is not None and t.requires_grad for t in tensors):
         raise ValueError(f"{name} records no gradient: call it under torch.no_grad() or on detached tensors "
-                         "(exemplar_rmsnorm_backward computes the norm's)")
+                         "(exemplar_rmsnorm_backward computes the norm's, exemplar_glu_backward the gated block's)")
 
 
 def _run(name, tensors, stream, *args):
@@ -566,6 +584,179 @@ def exemplar_mx_eval(V, sets, out=None, stream=None):
         raise ValueError("out must be float32 with l elements")
     _run("exemplar_mx_eval", (codes, scales, sets, out), stream, codes.data_ptr(), scales.data_ptr(), n, d, sets.data_ptr(),
          l, k, out.data_ptr())
+    return out
+
+
+class W4Rows(NamedTuple):
+    """Weights of ``n`` rows of ``d`` coordinates in 4 bits, with a scale and zero
+    point for ``group`` (32, 64 or 128) of them (the layout is in exemcl.h): uint8
+    ``codes`` (np/16 x dp/128 x 1024) and int32 ``words`` (np/16 x dp/group x 16), np
+    and dp the multiples of 16 and 128 that hold n and d."""
+    codes: Any
+    words: Any
+    n: int
+    d: int
+    group: int
+
+
+def _w4_check(q, name):
+    """Checks the tensors of W4Rows q and their sizes."""
+    import torch
+    codes, words, n, d, group = q
+    if group not in (32, 64, 128):
+        raise ValueError(f"{name}: groups have 32, 64 or 128 coordinates")
+    if n < 0 or not 1 <= d <= 1 << 22:
+        raise ValueError(f"{name}: rows have 1 to 2^22 coordinates, and there are not less than 0")
+    tiles, blocks = (n + 15) // 16, (d + 127) // 128
+    if codes.dtype != torch.uint8 or words.dtype != torch.int32 or codes.shape != (tiles, blocks, 1024) \
+            or words.shape != (tiles, blocks * 128 // group, 16):
+        raise ValueError(f"{name}: codes must be uint8 {tiles} x {blocks} x 1024 and words int32 "
+                         f"{tiles} x {blocks * 128 // group} x 16")
+
+
+def _bias_check(b, f, name):
+    import torch
+    if b is not None and (b.dtype != torch.float32 or b.shape != (f,)):
+        raise ValueError(f"{name} must be float32 with {f} elements")
+
+
+def _out(out, shape, dtype, device, stream):
+    """``out``, checked, or a new tensor."""
+    if out is None:
+        return _empty(stream)(shape, dtype=dtype, device=device)
+    if out.dtype != dtype or out.shape != shape:
+        raise ValueError(f"out must be a {shape[0]} x {shape[1]} tensor of {dtype}")
+    return out
+
+
+def exemplar_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, save=False, out=None, stream=None):
+    """(h, g, u): g = x Wg' + bg, u = x Wu' + bu, h = a(g) * u for x (n x d) and
+    weights of its type (f x d), biases in float32; g and u are kept for
+    exemplar_glu_backward where ``save``, else None (see exemplar_glu in
+    exemcl.h).  No autograd graph is recorded, and tensors that require a gradient
+    are refused outside torch.no_grad()."""
+    if x.dim() != 2 or Wg.dim() != 2:
+        raise ValueError("x must be n x d and Wg f x d")
+    dtype = x.dtype
+    prec = _precision(dtype)
+    n, d = x.shape
+    f = Wg.shape[0]
+    if Wg.dtype != dtype or Wu.dtype != dtype or Wg.shape[1] != d or Wu.shape != Wg.shape:
+        raise ValueError("Wg and Wu must have x's type, one shape and x's number of columns")
+    _bias_check(bg, f, "bg")
+    _bias_check(bu, f, "bu")
+    h = _out(out, (n, f), dtype, x.device, stream)
+    g = u = None
+    if save:
+        empty = _empty(stream)
+        g, u = empty((n, f), dtype=dtype, device=x.device), empty((n, f), dtype=dtype, device=x.device)
+    _run("exemplar_glu", (x, Wg, Wu, bg, bu, h), stream, x.data_ptr(), n, d, Wg.data_ptr(), Wu.data_ptr(), f, _at(bg),
+         _at(bu), prec, activation, h.data_ptr(), _at(g), _at(u))
+    return h, g, u
+
+
+def exemplar_glu_backward(dh, x, Wg, Wu, g, u, activation=EXEMCL_SILU, bias=False, stream=None):
+    """(dx, dWg, dWu, dbg, dbu) of exemplar_glu from the gradient dh of h and the g
+    and u it returned: dx and the weights' in x's type, the biases' in float32, None
+    unless ``bias`` (see exemplar_glu_backward in exemcl.h)."""
+    import torch
+    if x.dim() != 2 or Wg.dim() != 2:
+        raise ValueError("x must be n x d and Wg f x d")
+    dtype = x.dtype
+    prec = _precision(dtype)
+    n, d = x.shape
+    f = Wg.shape[0]
+    if Wg.dtype != dtype or Wu.dtype != dtype or Wg.shape[1] != d or Wu.shape != Wg.shape:
+        raise ValueError("Wg and Wu must have x's type, one shape and x's number of columns")
+    for t, name in ((dh, "dh"), (g, "g"), (u, "u")):
+        if t.dtype != dtype or t.shape != (n, f):
+            raise ValueError(f"{name} must have x's type and be n x f")
+    empty, like = (torch.empty, torch.empty_like) if stream is None else _empty_on(stream)
+    dx, dWg, dWu = like(x), like(Wg), like(Wu)
+    dbg = dbu = None
+    if bias:
+        dbg, dbu = empty(f, dtype=torch.float32, device=x.device), empty(f, dtype=torch.float32, device=x.device)
+    _run("exemplar_glu_backward", (x, dh, Wg, Wu, g, u), stream, dh.data_ptr(), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(),
+         g.data_ptr(), u.data_ptr(), n, d, f, prec, activation, dx.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), _at(dbg),
+         _at(dbu))
+    return dx, dWg, dWu, dbg, dbu
+
+
+def exemplar_w4_layout(n: int, d: int, group: int):
+    """(bytes of codes, number of words) of n rows of d coordinates; host only."""
+    cb, w = ctypes.c_int64(-1), ctypes.c_int64(-1)
+    rc = load().exemplar_w4_layout(n, d, group, ctypes.byref(cb), ctypes.byref(w))
+    if rc != EXEMCL_OK:
+        raise ExemclError(rc, "exemplar_w4_layout")
+    return int(cb.value), int(w.value)
+
+
+def exemplar_w4_quantize(w, group=128, stream=None):
+    """The rows of w (n x d) rounded to W4Rows (see exemplar_w4_quantize in exemcl.h)."""
+    import torch
+    if w.dim() != 2:
+        raise ValueError("w must be n x d")
+    prec = _precision(w.dtype)
+    n, d = w.shape
+    if group not in (32, 64, 128) or not 1 <= d <= 1 << 22:
+        raise ValueError("groups have 32, 64 or 128 coordinates, rows 1 to 2^22")
+    tiles, blocks = (n + 15) // 16, (d + 127) // 128
+    empty = _empty(stream)
+    q = W4Rows(empty((tiles, blocks, 1024), dtype=torch.uint8, device=w.device),
+               empty((tiles, blocks * 128 // group, 16), dtype=torch.int32, device=w.device), n, d, group)
+    _run("exemplar_w4_quantize", (w, q.codes, q.words), stream, w.data_ptr(), n, d, prec, group, q.codes.data_ptr(),
+         q.words.data_ptr())
+    return q
+
+
+def exemplar_w4_dequantize(q, dtype, out=None, stream=None):
+    """The values of W4Rows q as an n x d tensor of ``dtype``."""
+    prec = _precision(dtype)
+    _w4_check(q, "q")
+    out = _out(out, (q.n, q.d), dtype, q.codes.device, stream)
+    _run("exemplar_w4_dequantize", (q.codes, q.words, out), stream, q.codes.data_ptr(), q.words.data_ptr(), q.n, q.d,
+         q.group, prec, out.data_ptr())
+    return out
+
+
+def exemplar_w4_product(x, W, bias=None, out=None, stream=None):
+    """x W' + bias for x (n x d) and W4Rows W (f rows), as an n x f tensor of x's
+    type; the bias is float32 (see exemplar_w4_product in exemcl.h)."""
+    if x.dim() != 2:
+        raise ValueError("x must be n x d")
+    dtype = x.dtype
+    prec = _precision(dtype)
+    n, d = x.shape
+    _w4_check(W, "W")
+    codes, words, f, wd, group = W
+    if wd != d:
+        raise ValueError("x and W must have the same number of coordinates")
+    _bias_check(bias, f, "bias")
+    out = _out(out, (n, f), dtype, x.device, stream)
+    _run("exemplar_w4_product", (x, codes, words, bias, out), stream, x.data_ptr(), n, d, prec, codes.data_ptr(),
+         words.data_ptr(), f, group, _at(bias), out.data_ptr())
+    return out
+
+
+def exemplar_w4_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, out=None, stream=None):
+    """a(x Wg' + bg) * (x Wu' + bu) for x (n x d) and W4Rows of f rows with one group
+    size, as an n x f tensor of x's type (see exemplar_w4_glu in exemcl.h)."""
+    if x.dim() != 2:
+        raise ValueError("x must be n x d")
+    dtype = x.dtype
+    prec = _precision(dtype)
+    n, d = x.shape
+    _w4_check(Wg, "Wg")
+    _w4_check(Wu, "Wu")
+    f = Wg.n
+    if Wg.d != d or Wu.d != d or Wu.n != f or Wu.group != Wg.group:
+        raise ValueError("Wg and Wu must have x's number of coordinates, one number of rows and one group size")
+    _bias_check(bg, f, "bg")
+    _bias_check(bu, f, "bu")
+    out = _out(out, (n, f), dtype, x.device, stream)
+    _run("exemplar_w4_glu", (x, Wg.codes, Wg.words, Wu.codes, Wu.words, bg, bu, out), stream, x.data_ptr(), n, d, prec,
+         Wg.codes.data_ptr(), Wg.words.data_ptr(), Wu.codes.data_ptr(), Wu.words.data_ptr(), f, Wg.group, _at(bg), _at(bu),
+         activation, out.data_ptr())
     return out
 
 

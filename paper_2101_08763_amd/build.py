@@ -25,7 +25,9 @@ SOURCES = ["host.cpp", "kernels_mfma.hip", "kernels_mfma_f32.hip", "kernels_mfma
            "kernels_mfma_split_gather.hip", "kernels_mfma_split_gain_gather.hip", "kernels_mfma_split_rowmax.hip",
            "kernels_mfma_wide.hip", "kernels_mfma_bigd.hip", "kernels_aux.hip", "kernels_greedy.hip",
            "kernels_sqnorm.hip", "kernels_mx_rows.hip", "kernels_mx_product_fp4.hip", "kernels_mx_product_fp8.hip",
-           "kernels_mx_sets.hip", "kernels_mx_sets_short.hip", "kernels_mx_sets_wide.hip"]
+           "kernels_mx_sets.hip", "kernels_mx_sets_short.hip", "kernels_mx_sets_wide.hip",
+           "kernels_glu_rows.hip", "kernels_glu_point.hip", "kernels_glu_forward.hip", "kernels_glu_dx.hip",
+           "kernels_glu_dw.hip", "kernels_w4.hip", "kernels_w4_f32.hip", "kernels_w4_f16.hip", "kernels_w4_bf16.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-result", f"-I{INCLUDE}", f"-I{CSRC}"]
@@ -34,13 +36,14 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-fvisibility=h
 # The matrix-core kernels: accumulators in VGPRs (the epilogue reads them
 # directly), and max without NaN canonicalisation (inputs are finite).
 MFMA_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]
-# Norms and products keep NaN blocks.
+# Norms, products and the gated block keep NaN.
 MX_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 
 
 def _compile(src: str, verbose: bool) -> str:
     obj = os.path.join(OBJDIR, os.path.splitext(src)[0] + ".o")
-    extra = MFMA_FLAGS if src.startswith(("kernels_mfma_", "kernels_mx_sets")) else MX_FLAGS if src.startswith("kernels_mx_") else []
+    extra = MFMA_FLAGS if src.startswith(("kernels_mfma_", "kernels_mx_sets")) else \
+        MX_FLAGS if src.startswith(("kernels_mx_", "kernels_glu_", "kernels_w4")) else []
     cmd = [HIPCC, *FLAGS, *extra, "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
     if verbose:
         print(" ".join(cmd), flush=True)

@@ -15,6 +15,7 @@
 #include "exemcl.h"
 #include "internal.h"
 #include "mx_layout.hpp"
+#include "w4_layout.hpp"
 
 using namespace exemcl;
 
@@ -905,6 +906,120 @@ bool mx_rows_ok(const void *codes, const void *scales, int64_t n) {
     return n == 0 || (codes && scales && (uintptr_t)codes % 16 == 0 && (uintptr_t)scales % 4 == 0);
 }
 
+// ---------------------------------------------------------------------------
+// Gated feed-forward block.
+// ---------------------------------------------------------------------------
+constexpr int64_t kGluMaxD = int64_t(1) << 20;  // 256 rows within 31-bit byte offsets
+
+bool activation_ok(int a) { return a >= EXEMCL_SILU && a <= EXEMCL_RELU; }
+
+// Temporary memory that a call hands out piece by piece.
+struct Pieces {
+    int64_t bytes = 0;
+    char *base = nullptr;
+    int64_t take(int64_t b) {
+        const int64_t at = bytes;
+        bytes += align_up(b, 256);
+        return at;
+    }
+};
+
+// Rows as an operand of the tiled products: themselves, or laid out in temporary
+// memory.
+struct StagedRows {
+    const void *src = nullptr;
+    int64_t n = 0, d = 0, at = 0;
+    bool copied = false;
+    StagedRows() = default;
+    StagedRows(int prec, const void *p, int64_t rows, int64_t cols, Pieces *t)
+        : src(p), n(rows), d(cols), copied(!dense_in_place(prec, p, cols)) {
+        if (copied) at = t->take(n * dense_ld(d) * dense_planes(prec) * 2);
+    }
+    const void *ptr(const Pieces &t) const { return copied ? t.base + at : src; }
+    hipError_t stage(int prec, const Pieces &t, hipStream_t st) const {
+        return copied ? launch_dense_stage(prec, src, n, d, t.base + at, st) : hipSuccess;
+    }
+};
+
+int run_glu(const GluArgs &a, int prec, hipStream_t st) {
+    if (glu_takes_rows(prec, a.n, a.d, a.f)) return status_of(launch_glu_rows(prec, a, st));
+    Pieces t;
+    const StagedRows x(prec, a.x, a.n, a.d, &t), wg(prec, a.wg, a.f, a.d, &t), wu(prec, a.wu, a.f, a.d, &t);
+    Scratch ws;
+    if (t.bytes) {
+        const int rc = alloc_uncaptured(&ws, t.bytes, workspace_limit(), st);
+        if (rc) return rc;
+        t.base = (char *)ws.ptr;
+    }
+    for (const StagedRows *s : {&x, &wg, &wu})
+        if (s->stage(prec, t, st) != hipSuccess) return EXEMCL_EDEVICE;
+    const int64_t ld = dense_ld(a.d);
+    // (the two weights' planes are equally far apart)
+    const DenseArgs p{{x.ptr(t), nullptr, ld, a.n * ld}, {wg.ptr(t), wu.ptr(t), ld, a.f * ld}, a.n, a.f, a.d,
+                      a.bg, a.bu, a.act, a.h, nullptr, a.g, a.u};
+    return status_of(launch_glu_forward(prec, p, st));
+}
+
+struct GluGradArgs {
+    const void *dh, *x, *wg, *wu, *g, *u;
+    int64_t n, d, f;
+    int act;
+    void *dx, *dwg, *dwu;
+    float *dbg, *dbu;
+};
+
+int run_glu_grad(const GluGradArgs &a, int prec, hipStream_t st) {
+    const bool dw = a.dwg || a.dwu, db = a.dbg || a.dbu;
+    if (!a.dx && !dw && !db) return EXEMCL_OK;
+    Pieces t;
+    const int64_t ldd = dense_ld(a.d), ldf = dense_ld(a.f), planes = dense_planes(prec);
+    const int64_t dg = t.take(a.n * ldf * planes * 2), du = t.take(a.n * ldf * planes * 2);
+    const int64_t parts = glu_point_parts(a.n, a.f), sums = db ? t.take(2 * parts * a.f * 4) : 0;
+    StagedRows x, wg, wu;
+    if (dw) x = StagedRows(prec, a.x, a.n, a.d, &t);
+    if (a.dx) {
+        wg = StagedRows(prec, a.wg, a.f, a.d, &t);
+        wu = StagedRows(prec, a.wu, a.f, a.d, &t);
+    }
+    Scratch ws;
+    const int rc = alloc_uncaptured(&ws, t.bytes, workspace_limit(), st);
+    if (rc) return rc;
+    t.base = (char *)ws.ptr;
+    for (const StagedRows *s : {&x, &wg, &wu})
+        if (s->stage(prec, t, st) != hipSuccess) return EXEMCL_EDEVICE;
+    float *sum = db ? (float *)(t.base + sums) : nullptr;
+    const GluPointArgs p{a.dh, a.g, a.u, a.n, a.f, a.act, t.base + dg, t.base + du, parts, sum};
+    hipError_t e = launch_glu_point(prec, p, st);
+    if (e == hipSuccess && a.dx) {
+        const DenseArgs q{{t.base + dg, t.base + du, ldf, a.n * ldf}, {wg.ptr(t), wu.ptr(t), ldd, a.f * ldd},
+                          a.n, a.d, a.f, nullptr, nullptr, 0, a.dx, nullptr, nullptr, nullptr};
+        e = launch_glu_dx(prec, q, st);
+    }
+    if (e == hipSuccess && dw) {
+        const DenseArgs q{{t.base + dg, t.base + du, ldf, a.n * ldf}, {x.ptr(t), nullptr, ldd, a.n * ldd},
+                          a.f, a.d, a.n, nullptr, nullptr, 0, a.dwg, a.dwu, nullptr, nullptr};
+        e = launch_glu_dw(prec, q, st);
+    }
+    if (e == hipSuccess && a.dbg) e = launch_column_sum(sum, parts, a.f, a.dbg, st);
+    if (e == hipSuccess && a.dbu) e = launch_column_sum(sum + parts * a.f, parts, a.f, a.dbu, st);
+    return status_of(e);
+}
+
+// Without rows the sums over them are zeros.
+int zero_glu_grad(const GluGradArgs &a, int prec, hipStream_t st) {
+    hipError_t e = hipSuccess;
+    for (void *w : {a.dwg, a.dwu})
+        if (e == hipSuccess && w) e = launch_zero_bytes(w, a.f * a.d * elem_size(prec), st);
+    for (float *b : {a.dbg, a.dbu})
+        if (e == hipSuccess && b) e = launch_zero_bytes(b, a.f * 4, st);
+    return status_of(e);
+}
+
+bool w4_ok(const void *codes, const void *words, int64_t n) {
+    return n == 0 || (codes && words && (uintptr_t)codes % 16 == 0 && (uintptr_t)words % 16 == 0);
+}
+bool w4_group_ok(int group) { return group == 32 || group == 64 || group == 128; }
+
 }  // namespace
 
 extern "C" {
@@ -1268,6 +1383,75 @@ EXEMCL_API int exemplar_mx_eval(const void *codes, const void *scales, int64_t n
     if (d > kMxMaxD || !mx_rows_ok(codes, scales, n)) return EXEMCL_EINVAL;
     if (l > 0 && k > 0 && !sets) return EXEMCL_EINVAL;
     return run_mx_eval(codes, scales, n, d, sets, l, k, out, (hipStream_t)stream);
+}
+
+EXEMCL_API int exemplar_glu(const void *x, int64_t n, int64_t d, const void *Wg, const void *Wu, int64_t f,
+                            const float *bg, const float *bu, int precision, int activation, void *h, void *g, void *u,
+                            void *stream) {
+    if (!rows_ok(n, d, kGluMaxD) || f < 0 || f > kGluMaxD || !prec_ok(precision) || !activation_ok(activation))
+        return EXEMCL_EINVAL;
+    if (n == 0 || f == 0) return EXEMCL_OK;
+    if (!x || !Wg || !Wu || !h) return EXEMCL_EINVAL;
+    const GluArgs a{x, Wg, Wu, n, d, f, bg, bu, activation, h, g, u};
+    return run_glu(a, precision, (hipStream_t)stream);
+}
+
+EXEMCL_API int exemplar_glu_backward(const void *dh, const void *x, const void *Wg, const void *Wu, const void *g,
+                                     const void *u, int64_t n, int64_t d, int64_t f, int precision, int activation,
+                                     void *dx, void *dWg, void *dWu, float *dbg, float *dbu, void *stream) {
+    if (!rows_ok(n, d, kGluMaxD) || f < 0 || f > kGluMaxD || !prec_ok(precision) || !activation_ok(activation))
+        return EXEMCL_EINVAL;
+    const GluGradArgs a{dh, x, Wg, Wu, g, u, n, d, f, activation, dx, dWg, dWu, dbg, dbu};
+    hipStream_t st = (hipStream_t)stream;
+    if (f == 0) return dx && n ? status_of(launch_zero_bytes(dx, n * d * elem_size(precision), st)) : EXEMCL_OK;
+    if (n == 0) return zero_glu_grad(a, precision, st);
+    if (!dh || !g || !u || ((dWg || dWu) && !x) || (dx && (!Wg || !Wu))) return EXEMCL_EINVAL;
+    return run_glu_grad(a, precision, st);
+}
+
+EXEMCL_API int exemplar_w4_layout(int64_t n, int64_t d, int group, int64_t *code_bytes, int64_t *words) {
+    if (!rows_ok(n, d, kW4MaxD) || !w4_group_ok(group)) return EXEMCL_EINVAL;
+    if (code_bytes) *code_bytes = w4_tiles(n) * w4_blocks(d) * kW4Tile;
+    if (words) *words = w4_tiles(n) * w4_groups(d, group) * kW4Rows;
+    return EXEMCL_OK;
+}
+
+EXEMCL_API int exemplar_w4_quantize(const void *w, int64_t n, int64_t d, int precision, int group, void *codes,
+                                    uint32_t *words, void *stream) {
+    if (!rows_ok(n, d, kW4MaxD) || !prec_ok(precision) || !w4_group_ok(group)) return EXEMCL_EINVAL;
+    if ((n > 0 && !w) || !w4_ok(codes, words, n)) return EXEMCL_EINVAL;
+    return status_of(launch_w4_quantize(precision, w, n, d, group, codes, words, (hipStream_t)stream));
+}
+
+EXEMCL_API int exemplar_w4_dequantize(const void *codes, const uint32_t *words, int64_t n, int64_t d, int group,
+                                      int precision, void *w, void *stream) {
+    if (!rows_ok(n, d, kW4MaxD) || !prec_ok(precision) || !w4_group_ok(group)) return EXEMCL_EINVAL;
+    if ((n > 0 && !w) || !w4_ok(codes, words, n)) return EXEMCL_EINVAL;
+    return status_of(launch_w4_dequantize(precision, codes, words, n, d, group, w, (hipStream_t)stream));
+}
+
+EXEMCL_API int exemplar_w4_product(const void *x, int64_t n, int64_t d, int precision, const void *codes,
+                                   const uint32_t *words, int64_t f, int group, const float *bias, void *y, void *stream) {
+    if (!rows_ok(n, d, kW4MaxD) || !rows_ok(f, d, kW4MaxD) || !prec_ok(precision) || !w4_group_ok(group))
+        return EXEMCL_EINVAL;
+    if (!w4_ok(codes, words, f)) return EXEMCL_EINVAL;
+    if (n == 0 || f == 0) return EXEMCL_OK;
+    if (!x || !y) return EXEMCL_EINVAL;
+    const W4Args a{x, n, d, codes, words, nullptr, nullptr, f, group, bias, nullptr, 0, y};
+    return status_of(launch_w4_rows(precision, a, (hipStream_t)stream));
+}
+
+EXEMCL_API int exemplar_w4_glu(const void *x, int64_t n, int64_t d, int precision, const void *gate_codes,
+                               const uint32_t *gate_words, const void *up_codes, const uint32_t *up_words, int64_t f,
+                               int group, const float *bg, const float *bu, int activation, void *h, void *stream) {
+    if (!rows_ok(n, d, kW4MaxD) || !rows_ok(f, d, kW4MaxD) || !prec_ok(precision) || !w4_group_ok(group) ||
+        !activation_ok(activation))
+        return EXEMCL_EINVAL;
+    if (!w4_ok(gate_codes, gate_words, f) || !w4_ok(up_codes, up_words, f)) return EXEMCL_EINVAL;
+    if (n == 0 || f == 0) return EXEMCL_OK;
+    if (!x || !h) return EXEMCL_EINVAL;
+    const W4Args a{x, n, d, gate_codes, gate_words, up_codes, up_words, f, group, bg, bu, activation, h};
+    return status_of(launch_w4_rows(precision, a, (hipStream_t)stream));
 }
 
 EXEMCL_API int exemplar_plan(int64_t n, int64_t d, int64_t l, int64_t k, int precision, int *path,

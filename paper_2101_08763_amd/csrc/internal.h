@@ -280,4 +280,85 @@ hipError_t launch_mx_sets(const void *codes, const void *scales, int64_t n, int6
 int64_t mx_sets_folds(int64_t G);
 hipError_t launch_mx_fold(const float *partials, int64_t G, int64_t lpad, int64_t l, float *folded, hipStream_t st);
 
+// ---------------------------------------------------------------------------
+// Gated feed-forward block and 4-bit weights with group scales (w4_layout.hpp).
+// ---------------------------------------------------------------------------
+enum Activation { ACT_SILU = 0, ACT_GELU = 1, ACT_GELU_TANH = 2, ACT_RELU = 3 };
+
+// h = a(g) u, g = x Wg' + bg, u = x Wu' + bu; bg, bu, g and u nullable.
+struct GluArgs {
+    const void *x, *wg, *wu;
+    int64_t n, d, f;
+    const float *bg, *bu;
+    int act;
+    void *h, *g, *u;
+};
+// Few rows: the weights straight from memory, in any alignment; no temporary
+// memory.
+bool glu_takes_rows(int prec, int64_t n, int64_t d, int64_t f);
+hipError_t launch_glu_rows(int prec, const GluArgs &a, hipStream_t st);
+
+// Weights of 4 bits: y = x W' + b, or the block on two of them (wu not null).
+struct W4Args {
+    const void *x;
+    int64_t n, d;
+    const void *wg, *wg_words, *wu, *wu_words;
+    int64_t f;
+    int group;
+    const float *bg, *bu;
+    int act;
+    void *y;
+};
+hipError_t launch_w4_rows(int prec, const W4Args &a, hipStream_t st);
+hipError_t launch_w4_quantize(int prec, const void *w, int64_t n, int64_t d, int group, void *codes, void *words,
+                              hipStream_t st);
+hipError_t launch_w4_dequantize(int prec, const void *codes, const void *words, int64_t n, int64_t d, int group, void *w,
+                                hipStream_t st);
+
+// Tiled products.  An operand's rows are `ld` elements, a multiple of 8, at
+// 16-byte aligned addresses, in one plane or (fp32) three of bf16 parts, `plane`
+// elements apart; what is between a row's own elements and ld is zeros.
+struct DenseOperand {
+    const void *p, *p2;  // p2: the second matrix's (nullable)
+    int64_t ld, plane;
+};
+struct DenseArgs {
+    DenseOperand A, B;
+    int64_t M, N, K;
+    const float *bg, *bu;
+    int act;
+    void *C, *C2, *g, *u;
+};
+int64_t dense_ld(int64_t d);
+int dense_planes(int prec);
+// Whether rows of d elements at p are an operand as they are.
+bool dense_in_place(int prec, const void *p, int64_t d);
+// Rows of d elements as an operand (rows x dense_ld(d) elements a plane).
+hipError_t launch_dense_stage(int prec, const void *src, int64_t n, int64_t d, void *dst, hipStream_t st);
+// h (C), g and u of n rows: A = x, B = Wg and Wu.
+hipError_t launch_glu_forward(int prec, const DenseArgs &a, hipStream_t st);
+// C = A B + A2 B2: M x K times K x N.
+hipError_t launch_glu_dx(int prec, const DenseArgs &a, hipStream_t st);
+// C = A' B, C2 = A2' B (each nullable): A is K x M, B K x N.
+hipError_t launch_glu_dw(int prec, const DenseArgs &a, hipStream_t st);
+
+// dg = dh u a'(g) and du = dh a(g) as operands, and the sums of their columns over
+// the rows of each part: sums is 2 x parts x f (nullable).
+struct GluPointArgs {
+    const void *dh, *g, *u;
+    int64_t n, f;
+    int act;
+    void *dg, *du;
+    int64_t parts;
+    float *sums;
+};
+int64_t glu_point_parts(int64_t n, int64_t f);
+hipError_t launch_glu_point(int prec, const GluPointArgs &a, hipStream_t st);
+
+// `bytes` (an even number) zero bytes at p.
+hipError_t launch_zero_bytes(void *p, int64_t bytes, hipStream_t st);
+
+// out[c] = sum over g < G of partial[g * d + c], in 64 bits, in a fixed order.
+hipError_t launch_column_sum(const float *partial, int64_t G, int64_t d, float *out, hipStream_t st);
+
 }  // namespace exemcl

@@ -472,12 +472,16 @@ hipError_t grad_typed(const NormGradArgs &a, hipStream_t st) {
         }
     }
     if (e != hipSuccess || !a.dw) return e;
-    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((a.d + kDwCols - 1) / kDwCols)), dim3(kDwCols * kDwRows), 0, st,
-                       a.partial, (int)a.parts, (int)a.d, a.dw);
-    return hipGetLastError();
+    return launch_column_sum(a.partial, a.parts, a.d, a.dw, st);
 }
 
 }  // namespace
+
+hipError_t launch_column_sum(const float *partial, int64_t G, int64_t d, float *out, hipStream_t st) {
+    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((d + kDwCols - 1) / kDwCols)), dim3(kDwCols * kDwRows), 0, st,
+                       partial, (int)G, (int)d, out);
+    return hipGetLastError();
+}
 
 hipError_t launch_mx_quantize(int prec, int bits, const void *x, int64_t n, int64_t d, void *codes, void *scales,
                               hipStream_t st) {

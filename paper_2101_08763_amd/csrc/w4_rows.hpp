@@ -1,0 +1,27 @@
+// w4_rows.hpp -- products by 4-bit weights and the gated block on them: the sizes'
+// kernels (instantiated in kernels_w4_*.hip, one per type of the rows).
+#pragma once
+
+#include "glu_rows.hpp"
+
+namespace exemcl {
+
+template <typename T, int GROUP, bool GLU>
+hipError_t w4_sized(const RowsArgs &r, hipStream_t st) {
+    if (r.n <= 16) return rows_launch<T, GROUP, GLU, 1, 1>(r, st);
+    return rows_launch<T, GROUP, GLU, GLU ? 1 : 2, 4>(r, st);
+}
+
+template <typename T>
+hipError_t w4_typed(const W4Args &a, hipStream_t st) {
+    const RowsArgs r{a.x, a.n, a.d, {a.wg, a.wu}, {a.wg_words, a.wu_words}, a.f, {a.bg, a.bu}, a.act, a.y, nullptr, nullptr, 0, 0};
+    if (a.group == 32) return a.wu ? w4_sized<T, 32, true>(r, st) : w4_sized<T, 32, false>(r, st);
+    if (a.group == 64) return a.wu ? w4_sized<T, 64, true>(r, st) : w4_sized<T, 64, false>(r, st);
+    return a.wu ? w4_sized<T, 128, true>(r, st) : w4_sized<T, 128, false>(r, st);
+}
+
+hipError_t w4_run_f32(const W4Args &a, hipStream_t st);
+hipError_t w4_run_f16(const W4Args &a, hipStream_t st);
+hipError_t w4_run_bf16(const W4Args &a, hipStream_t st);
+
+}  // namespace exemcl
