@@ -67,6 +67,36 @@ __device__ __forceinline__ int across_swap(int t) {
 // the other fragment.
 __device__ __forceinline__ int first_row(int lr, int j) { return 8 * (lr >> 2) + 4 * (j ^ (lr >> 2 & 1)) + (lr & 3); }
 
+// A value that is the same in all lanes, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+template <typename E>
+__device__ __forceinline__ const E *uniform(const E *p) {
+    const uint64_t v = (uint64_t)p;
+    return (const E *)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
+// Eight reads of 8 bytes that transpose 4 steps of 4 x 4 rows, for two fragments of
+// 16 rows x 2 x 32 steps; ROW: bytes of a step.  They are written out, with their
+// wait, because the compiler waits for all copies to LDS before a transposing read.
+typedef uint32_t u32x2t __attribute__((ext_vector_type(2)));
+template <int ROW>
+__device__ __forceinline__ void read_across(uint32_t at0, uint32_t at1, u32x2t (&v)[2][2][2]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\t"
+        "ds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %4, %9\n\t"
+        "ds_read_b64_tr_b16 %5, %9 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %2, %8 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %3, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %6, %9 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0][0][0]), "=&v"(v[0][0][1]), "=&v"(v[0][1][0]), "=&v"(v[0][1][1]), "=&v"(v[1][0][0]), "=&v"(v[1][0][1]),
+          "=&v"(v[1][1][0]), "=&v"(v[1][1][1])
+        : "v"(at0), "v"(at1), "n"(4 * ROW), "n"(32 * ROW), "n"(36 * ROW)
+        : "memory");
+}
+
 template <typename T, int LA, int LB, int EPI, int AF>
 __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
     using P = DensePlan<AF>;
@@ -76,52 +106,54 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
     constexpr int PRODUCTS = Operand<T>::PRODUCTS, BK = P::BK;
     extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
+    const int wave = uniform(tid >> 6), wm = wave >> 2, wn = wave & 3;
 
     // Workgroups b, b + 8, b + 16, ... share an XCD and its L2: they take
     // consecutive tiles, up to 8 of one row of tiles side by side.
-    const int64_t mblocks = (int64_t)a.mblocks * a.pairs, units = mblocks * a.nblocks, per = (units + 7) / 8;
-    const int64_t wg = flat_block(), pos = wg >> 3, un = (wg & 7) * per + pos;
+    const int mblocks = a.mblocks * a.pairs, units = mblocks * a.nblocks, per = (units + 7) / 8;
+    const int wg = (int)flat_block(), pos = wg >> 3, un = (wg & 7) * per + pos;
     if (pos >= per || un >= units) return;
-    const int64_t strip = un / (mblocks * 8);
-    const int width = (int)min((int64_t)8, a.nblocks - strip * 8);
-    const int64_t in = un - strip * mblocks * 8;
-    const int64_t mt = in / width;
-    const bool other = mt >= a.mblocks;  // results of A2
-    const int64_t m0 = (mt - (other ? a.mblocks : 0)) * P::BM;
-    const int64_t n0 = (strip * 8 + in % width) * (EPI == GLU ? P::BN / 2 : P::BN);
+    const int strip = uniform((uint32_t)un / (uint32_t)(mblocks * 8)), width = min(8, a.nblocks - strip * 8);
+    const int in = un - strip * mblocks * 8;
+    const int mt = uniform((uint32_t)in / (uint32_t)width), nt = strip * 8 + in - mt * width;
+    const int other = mt >= a.mblocks ? 1 : 0;  // results of A2
+    const int m0 = (mt - (other ? a.mblocks : 0)) * P::BM, n0 = nt * (EPI == GLU ? P::BN / 2 : P::BN);
+    const int lda = (int)a.lda, ldb = (int)a.ldb;
+    const uint32_t K = (uint32_t)a.K;  // below 2^31
+    const int mrows = min(P::BM, (int)a.M - m0), nrows = min(EPI == GLU ? P::BN / 2 : P::BN, (int)a.N - n0);
 
-    // Stages: for every matrix and product of parts, K in steps of 64.
-    const int ksteps = (int)((a.K + BK - 1) / BK), stages = ksteps * PRODUCTS * a.matrices;
-    const E *at, *bt, *bt2;  // the pair's operands, from this tile's rows on
-    auto pair = [&](int s) {
-        const int mat = s / PRODUCTS, p = s - mat * PRODUCTS;
-        at = (const E *)((mat | (int)other) ? a.A2 : a.A) + (PRODUCTS > 1 ? part_a(p) * a.plane_a : 0);
-        bt = (const E *)(mat ? a.B2 : a.B) + (PRODUCTS > 1 ? part_b(p) * a.plane_b : 0);
-        at += LA == ALONG ? m0 * a.lda : m0;
-        if constexpr (EPI == GLU) bt2 = (const E *)a.B2 + (PRODUCTS > 1 ? part_b(p) * a.plane_b : 0) + n0 * a.ldb;
-        bt += LB == ALONG ? n0 * a.ldb : n0;
+    // Stages: for every pair of a matrix and a product of parts, K in steps of 64.
+    // The products of small parts come first, while the sums are small.
+    const int pairs = PRODUCTS * a.matrices, stages = (int)((K + BK - 1) / BK) * pairs;
+    const E *at = nullptr, *bt = nullptr, *bt2 = nullptr;  // the operands of the stage to issue next
+    int is_pair = 0;
+    uint32_t is_k = 0;
+    auto pair = [&]() {
+        const int mat = is_pair / PRODUCTS, p = PRODUCTS - 1 - (is_pair - mat * PRODUCTS);
+        const int64_t pa = PRODUCTS > 1 ? part_a(p) * a.plane_a : 0, pb = PRODUCTS > 1 ? part_b(p) * a.plane_b : 0;
+        at = uniform((const E *)((mat | other) ? a.A2 : a.A) + pa + (LA == ALONG ? (int64_t)m0 * lda : m0));
+        bt = uniform((const E *)(mat ? a.B2 : a.B) + pb + (LB == ALONG ? (int64_t)n0 * ldb : n0));
+        if constexpr (EPI == GLU) bt2 = uniform((const E *)a.B2 + pb + (int64_t)n0 * ldb);
     };
-    pair(0);
-    int is_pair = 0, is_k = 0;  // the stage to issue next
+    pair();
 
     // What a thread copies of a region: a chunk of 16 bytes per load.  `off` is
     // its place in the window of the first half, `t` its first step of t.
     uint32_t a_off[P::A_LOADS], b_off[P::B_LOADS];
-    int a_t[P::A_LOADS], b_t[P::B_LOADS];
+    uint32_t a_t[P::A_LOADS], b_t[P::B_LOADS];
 #pragma unroll
     for (int i = 0; i < P::A_LOADS; ++i) {
         const int q = (wave * P::A_LOADS + i) * 64 + lane;
         if constexpr (LA == ALONG) {
             const int p = q / 8, c = (q % 8) ^ along_swap(p);
             const int row = p / (16 * AF) * (32 * AF) + p % (16 * AF);
-            a_off[i] = (uint32_t)(row * (int)a.lda + c * 8) * 2;
+            a_off[i] = (uint32_t)(row * lda + c * 8) * 2;
             a_t[i] = c * 8;
         } else {
             constexpr int CHUNKS = P::A_ROWS / 8;
             const int t = q / CHUNKS, e = ((q % CHUNKS) ^ across_swap<false, CHUNKS>(t)) * 8;
             const int row = e / (16 * AF) * (32 * AF) + e % (16 * AF);
-            a_off[i] = (uint32_t)(t * (int)a.lda + row) * 2;
+            a_off[i] = (uint32_t)(t * lda + row) * 2;
             a_t[i] = t;
         }
     }
@@ -132,97 +164,104 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
         if constexpr (LB == ALONG) {
             const int p = q / 8, c = (q % 8) ^ along_swap(p);
             const int row = p / 32 * APART + first_row(p % 16, p / 16 % 2);
-            b_off[i] = (uint32_t)(row * (int)a.ldb + c * 8) * 2;
+            b_off[i] = (uint32_t)(row * ldb + c * 8) * 2;
             b_t[i] = c * 8;
         } else {
             const int t = q / 16, e = ((q % 16) ^ across_swap<true, 16>(t)) * 8;
-            b_off[i] = (uint32_t)(t * (int)a.ldb + e / 32 * APART + e % 32) * 2;
+            b_off[i] = (uint32_t)(t * ldb + e / 32 * APART + e % 32) * 2;
             b_t[i] = t;
         }
     }
-    // Copies of half h of a stage's A or B into the buffer at `to`.  ALONG: the
-    // window is the tile's rows, and a chunk past K is dead; ACROSS: it is the
-    // steps of t that are left.
-    auto issue_a = [&](int h, int to) {
-        const int64_t k0 = (int64_t)is_k * BK;
-        const bool live = is_pair < PRODUCTS * a.matrices;
-        const E *base = LA == ALONG ? at : at + k0 * a.lda;
-        const int64_t rows = LA == ALONG ? min((int64_t)P::BM, a.M - m0) : min((int64_t)BK, a.K - k0);
-        const int64_t bytes = (rows * a.lda - (LA == ALONG ? 0 : m0)) * 2;
-        const auto win = window_rsrc(base, live ? (uint32_t)max((int64_t)0, bytes) : 0u);
+    // Copies of half h of the stage's A or B into buffer `buf`.  ALONG: the window
+    // is the tile's rows, and a chunk past K is dead; ACROSS: it is the steps of t
+    // that are left.  Past the last stage the window is empty.
+    auto issue_a = [&](int h, int buf) {
+        uint32_t bytes = LA == ALONG ? (uint32_t)mrows * (uint32_t)lda * 2 : (min((uint32_t)BK, K - is_k) * (uint32_t)lda - (uint32_t)m0) * 2;
+        if (is_pair >= pairs) bytes = 0;
+        const auto win = window_rsrc(at, bytes);
 #pragma unroll
         for (int i = 0; i < P::A_LOADS; ++i) {
-            uint32_t off = a_off[i];
-            if constexpr (LA == ALONG)
-                off = k0 + a_t[i] < a.K ? off + (uint32_t)(k0 * 2) + (uint32_t)(h * 16 * AF * (int)a.lda * 2) : kDeadOffset;
-            else
-                off += h * 16 * AF * 2;
-            window_to_lds16(win, smem + to + h * P::A_REGION + (wave * P::A_LOADS + i) * 1024, off);
+            uint32_t off = a_off[i] + (uint32_t)(LA == ALONG ? h * 16 * AF * lda * 2 + is_k * 2 : h * 16 * AF * 2);
+            if constexpr (LA == ALONG) off = is_k + a_t[i] < K ? off : kDeadOffset;
+            window_to_lds16(win, smem + buf * P::STAGE + h * P::A_REGION + (wave * P::A_LOADS + i) * 1024, off);
         }
     };
-    auto issue_b = [&](int h, int to) {
-        const int64_t k0 = (int64_t)is_k * BK;
-        const bool live = is_pair < PRODUCTS * a.matrices;
-        const E *base = EPI == GLU && h ? bt2 : LB == ALONG ? bt : bt + k0 * a.ldb;
-        const int64_t rows = LB == ALONG ? min((int64_t)(EPI == GLU ? P::BN / 2 : P::BN), a.N - n0) : min((int64_t)BK, a.K - k0);
-        const int64_t bytes = (rows * a.ldb - (LB == ALONG ? 0 : n0)) * 2;
-        const auto win = window_rsrc(base, live ? (uint32_t)max((int64_t)0, bytes) : 0u);
+    auto issue_b = [&](int h, int buf) {
+        uint32_t bytes = LB == ALONG ? (uint32_t)nrows * (uint32_t)ldb * 2 : (min((uint32_t)BK, K - is_k) * (uint32_t)ldb - (uint32_t)n0) * 2;
+        if (is_pair >= pairs) bytes = 0;
+        const auto win = window_rsrc(EPI == GLU && h ? bt2 : bt, bytes);
+        const int half = EPI == GLU ? 0 : h;
 #pragma unroll
         for (int i = 0; i < P::B_LOADS; ++i) {
-            uint32_t off = b_off[i];
-            const int half = EPI == GLU ? 0 : h;
-            if constexpr (LB == ALONG)
-                off = k0 + b_t[i] < a.K ? off + (uint32_t)(k0 * 2) + (uint32_t)(half * 32 * (int)a.ldb * 2) : kDeadOffset;
-            else
-                off += half * 32 * 2;
-            window_to_lds16(win, smem + to + 2 * P::A_REGION + h * P::B_REGION + (wave * P::B_LOADS + i) * 1024, off);
+            uint32_t off = b_off[i] + (uint32_t)(LB == ALONG ? half * 32 * ldb * 2 + is_k * 2 : half * 32 * 2);
+            if constexpr (LB == ALONG) off = is_k + b_t[i] < K ? off : kDeadOffset;
+            window_to_lds16(win, smem + buf * P::STAGE + 2 * P::A_REGION + h * P::B_REGION + (wave * P::B_LOADS + i) * 1024, off);
         }
     };
     auto issued = [&]() {
-        if (++is_k == ksteps) {
+        is_k += BK;
+        if constexpr (LA == ACROSS) at += (int64_t)BK * lda;
+        if constexpr (LB == ACROSS) bt += (int64_t)BK * ldb;
+        if (is_k >= K) {
             is_k = 0;
-            if (++is_pair < PRODUCTS * a.matrices) pair(is_pair);
+            if (++is_pair < pairs) pair();
         }
     };
 
     // Operands of one half from LDS, fragments of 16 rows x 32 steps.
-    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-    auto across = [&](int byte, int row_bytes) {
-        const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(smem + byte));
-        const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(smem + byte + 4 * row_bytes));
-        return __builtin_bit_cast(vec, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    vec av[AF][2], bv[2][2][2];  // [fragment][step]; B's of both halves
-    auto read_a = [&](int h, int from) {
-        const int region = from + h * P::A_REGION;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+    auto join = [](u32x2t lo, u32x2t hi) { return __builtin_bit_cast(vec, u32x4{lo[0], lo[1], hi[0], hi[1]}); };
+    vec av[AF][2], bv[3][2][2];  // [fragment][32 steps]; B's second half, and the first one's of both buffers
+    auto read_a = [&](int h, int buf) {
+        const int region = buf * P::STAGE + h * P::A_REGION;
+        if constexpr (LA == ALONG) {
 #pragma unroll
-        for (int w = 0; w < AF; ++w)
+            for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                if constexpr (LA == ALONG) {
+                for (int w = 0; w < AF; ++w) {
                     const int p = wm * 16 * AF + w * 16 + lr;
                     av[w][ks] = *reinterpret_cast<const vec *>(smem + region + p * 128 + ((ks * 4 + g) ^ along_swap(lr)) * 16);
-                } else {
-                    constexpr int CHUNKS = P::A_ROWS / 8;
-                    const int t = ks * 32 + 8 * g + (lr >> 2), c = wm * 2 * AF + w * 2 + (lr >> 1 & 1);
-                    av[w][ks] = across(region + t * CHUNKS * 16 + (c ^ across_swap<false, CHUNKS>(t)) * 16 + (lr & 1) * 8, CHUNKS * 16);
                 }
+        } else {
+            constexpr int CHUNKS = P::A_ROWS / 8;
+            const int t = 8 * g + (lr >> 2);
+#pragma unroll
+            for (int w = 0; w < AF; w += 2) {
+                uint32_t from[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int c = wm * 2 * AF + (w + e) * 2 + (lr >> 1 & 1);
+                    from[e] = lds + region + t * CHUNKS * 16 + (c ^ across_swap<false, CHUNKS>(t)) * 16 + (lr & 1) * 8;
+                }
+                u32x2t v[2][2][2];
+                read_across<CHUNKS * 16>(from[0], from[1], v);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks) av[w + e][ks] = join(v[e][ks][0], v[e][ks][1]);
             }
+        }
     };
-    auto read_b = [&](int h, int from) {
-        const int region = from + 2 * P::A_REGION + h * P::B_REGION;
+    auto read_b = [&](int h, int buf, vec(&to)[2][2]) {
+        const int region = buf * P::STAGE + 2 * P::A_REGION + h * P::B_REGION;
+        if constexpr (LB == ALONG) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+            for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                if constexpr (LB == ALONG) {
+                for (int j = 0; j < 2; ++j) {
                     const int p = wn * 32 + j * 16 + lr;
-                    bv[h][j][ks] = *reinterpret_cast<const vec *>(smem + region + p * 128 + ((ks * 4 + g) ^ along_swap(lr)) * 16);
-                } else {
-                    const int t = ks * 32 + 8 * g + (lr >> 2), c = wn * 4 + (lr & 3);
-                    bv[h][j][ks] = across(region + t * 256 + (c ^ across_swap<true, 16>(t)) * 16 + (j ^ (lr & 1)) * 8, 256);
+                    to[j][ks] = *reinterpret_cast<const vec *>(smem + region + p * 128 + ((ks * 4 + g) ^ along_swap(lr)) * 16);
                 }
-            }
+        } else {
+            const int t = 8 * g + (lr >> 2), c = wn * 4 + (lr & 3);
+            const uint32_t from = lds + region + t * 256 + (c ^ across_swap<true, 16>(t)) * 16 + (lr & 1) * 8;
+            u32x2t v[2][2][2];
+            read_across<256>(from, from ^ 8, v);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) to[j][ks] = join(v[j][ks][0], v[j][ks][1]);
+        }
     };
     f32x4 acc[2][AF][2][2];
 #pragma unroll
@@ -233,37 +272,71 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
             for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) acc[ha][w][hb][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    auto multiply = [&](int ha, int hb) {
+
+    // A phase: reads for one quarter of the tile and copies for the stage after
+    // next, then the quarter's instructions.  The wavefronts 0 .. 3 are half a phase
+    // ahead of 4 .. 7, with which they share the SIMDs: while one reads, the other
+    // multiplies.  What is read in a phase has been waited for, by every wavefront,
+    // in the one before it; the copies go to the region that was read there.
+    auto ready = [&]() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * (P::A_LOADS + P::B_LOADS)) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](int ha, int hb, const vec(&b)[2][2]) {
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int w = 0; w < AF; ++w)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc[ha][w][hb][j] = M::mma(bv[hb][j][ks], av[w][ks], 0, acc[ha][w][hb][j]);
+                for (int j = 0; j < 2; ++j) acc[ha][w][hb][j] = M::mma(b[j][ks], av[w][ks], 0, acc[ha][w][hb][j]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
     };
-
-    auto issue = [&](int to) {
-        issue_a(0, to);
-        issue_b(0, to);
-        issue_b(1, to);
-        issue_a(1, to);
+    auto stage = [&](auto parity) {
+        constexpr int buf = decltype(parity)::value;
+        read_a(0, buf);
+        issue_b(0, buf);
+        ready();
+        multiply(0, 0, bv[1 + buf]);
+        read_b(1, buf, bv[0]);
+        issue_a(0, buf);
+        ready();
+        multiply(0, 1, bv[0]);
+        read_a(1, buf);
+        issue_b(1, buf);
+        ready();
+        multiply(1, 1, bv[0]);
+        read_b(0, 1 - buf, bv[2 - buf]);
+        issue_a(1, buf);
         issued();
+        ready();
+        multiply(1, 0, bv[1 + buf]);
     };
-    issue(0);
-    for (int st = 0; st < stages; ++st) {
-        const int from = (st & 1) * P::STAGE;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        issue(P::STAGE - from);
-        read_a(0, from);
-        read_b(0, from);
-        read_b(1, from);
-        multiply(0, 0);
-        multiply(0, 1);
-        read_a(1, from);
-        multiply(1, 0);
-        multiply(1, 1);
+#pragma unroll
+    for (int buf = 0; buf < 2; ++buf) {
+        issue_b(0, buf);
+        issue_a(0, buf);
+        issue_b(1, buf);
+        issue_a(1, buf);
+        issued();
     }
+    ready();
+    read_b(0, 0, bv[1]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    if (wave >= 4) __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    for (int st = 0; st < stages; st += 2) {
+        stage(std::integral_constant<int, 0>());
+        if (st + 1 < stages) stage(std::integral_constant<int, 1>());
+    }
+    if (wave < 4) __builtin_amdgcn_s_barrier();
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
 
     // Row w * 16 + lr of a quarter, and its columns 8 g .. 8 g + 7: fragment g % 2
