@@ -2,14 +2,15 @@
 // kernels (instantiated in kernels_w4_*.hip, one per type of the rows).
 #pragma once
 
-#include "glu_rows.hpp"
+#include "w4_tile.hpp"
 
 namespace exemcl {
 
 template <typename T, int GROUP, bool GLU>
 hipError_t w4_sized(const RowsArgs &r, hipStream_t st) {
     if (r.n <= 16) return rows_launch<T, GROUP, GLU, 1, 1>(r, st);
-    return rows_launch<T, GROUP, GLU, GLU ? 1 : 2, 4>(r, st);
+    if (r.n <= 64) return rows_launch<T, GROUP, GLU, GLU ? 1 : 2, 4>(r, st);
+    return w4_tile_launch<T, GROUP, GLU>(r, st);
 }
 
 template <typename T>

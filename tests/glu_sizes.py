@@ -12,4 +12,4 @@ LARGE = [(4100, 40, 2060), (4100, 2090, 130), (130, 1300, 2900)]
 
 # Products by 4-bit weights (n, d, f).
 W4 = [(1, 1, 1), (1, 40, 300), (1, 1301, 77), (3, 129, 33), (7, 2000, 15), (16, 128, 130), (17, 64, 257), (33, 7, 19),
-      (64, 520, 100), (65, 384, 100), (200, 301, 70)]
+      (64, 520, 100), (65, 384, 100), (200, 301, 70), (300, 1000, 530)]
