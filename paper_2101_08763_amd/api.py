@@ -414,21 +414,35 @@ def _check_gradient(name, tensors):
                          "(exemplar_rmsnorm_backward computes the norm's, exemplar_glu_backward the gated block's)")
 
 
+_DEVICE_QUERIES = None  # (current device, its current raw stream), where PyTorch has them
+
+
+def _device_queries():
+    global _DEVICE_QUERIES
+    if _DEVICE_QUERIES is None:
+        import torch
+        _DEVICE_QUERIES = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
+                           getattr(torch._C, "_cuda_getCurrentRawStream",
+                                   lambda dev: torch.cuda.current_stream(dev).cuda_stream))
+    return _DEVICE_QUERIES
+
+
 def _run(name, tensors, stream, *args):
     """Call ``name`` of the library on the device of ``tensors`` (the first
     one's; None: not given) with ``args`` and the stream, and raise its error.
     The checks and messages are _check_device's; the calls on rows can be a few
     microseconds each, so the common case takes the short way."""
-    import torch
     dev = tensors[0].get_device()
     for t in tensors:
         if t is not None and (dev < 0 or t.get_device() != dev or not t.is_contiguous() or t.requires_grad):
             _check_gradient(name, tensors)
             _check_device(*tensors)
     fn = getattr(_LIB or load(), name)
-    if dev == torch.cuda.current_device():
-        rc = fn(*args, _stream(stream))
+    current_device, raw_stream = _DEVICE_QUERIES or _device_queries()
+    if dev == current_device():
+        rc = fn(*args, raw_stream(dev) if stream is None else _stream(stream))
     else:
+        import torch
         with torch.cuda.device(dev):
             rc = fn(*args, _stream(stream))
     if stream is not None:
@@ -601,29 +615,42 @@ class W4Rows(NamedTuple):
 
 def _w4_check(q, name):
     """Checks the tensors of W4Rows q and their sizes."""
-    import torch
     codes, words, n, d, group = q
-    if group not in (32, 64, 128):
+    if group != 128 and group != 64 and group != 32:
         raise ValueError(f"{name}: groups have 32, 64 or 128 coordinates")
     if n < 0 or not 1 <= d <= 1 << 22:
         raise ValueError(f"{name}: rows have 1 to 2^22 coordinates, and there are not less than 0")
     tiles, blocks = (n + 15) // 16, (d + 127) // 128
-    if codes.dtype != torch.uint8 or words.dtype != torch.int32 or codes.shape != (tiles, blocks, 1024) \
+    uint8, int32 = _W4_TYPES or _w4_types()
+    if codes.dtype != uint8 or words.dtype != int32 or codes.shape != (tiles, blocks, 1024) \
             or words.shape != (tiles, blocks * 128 // group, 16):
         raise ValueError(f"{name}: codes must be uint8 {tiles} x {blocks} x 1024 and words int32 "
                          f"{tiles} x {blocks * 128 // group} x 16")
 
 
-def _bias_check(b, f, name):
+_W4_TYPES = None
+
+
+def _w4_types():
+    global _W4_TYPES
     import torch
-    if b is not None and (b.dtype != torch.float32 or b.shape != (f,)):
+    _W4_TYPES = (torch.uint8, torch.int32)
+    return _W4_TYPES
+
+
+def _bias_check(b, f, name):
+    if b is None:
+        return
+    import torch
+    if b.dtype != torch.float32 or b.shape != (f,):
         raise ValueError(f"{name} must be float32 with {f} elements")
 
 
-def _out(out, shape, dtype, device, stream):
-    """``out``, checked, or a new tensor."""
+def _out(out, shape, x, stream):
+    """``out``, checked, or a new tensor, of x's type and device."""
+    dtype = x.dtype
     if out is None:
-        return _empty(stream)(shape, dtype=dtype, device=device)
+        return x.new_empty(shape) if stream is None else _empty(stream)(shape, dtype=dtype, device=x.device)
     if out.dtype != dtype or out.shape != shape:
         raise ValueError(f"out must be a {shape[0]} x {shape[1]} tensor of {dtype}")
     return out
@@ -645,11 +672,10 @@ def exemplar_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, save=False
         raise ValueError("Wg and Wu must have x's type, one shape and x's number of columns")
     _bias_check(bg, f, "bg")
     _bias_check(bu, f, "bu")
-    h = _out(out, (n, f), dtype, x.device, stream)
+    h = _out(out, (n, f), x, stream)
     g = u = None
     if save:
-        empty = _empty(stream)
-        g, u = empty((n, f), dtype=dtype, device=x.device), empty((n, f), dtype=dtype, device=x.device)
+        g, u = _out(None, (n, f), x, stream), _out(None, (n, f), x, stream)
     _run("exemplar_glu", (x, Wg, Wu, bg, bu, h), stream, x.data_ptr(), n, d, Wg.data_ptr(), Wu.data_ptr(), f, _at(bg),
          _at(bu), prec, activation, h.data_ptr(), _at(g), _at(u))
     return h, g, u
@@ -713,7 +739,10 @@ def exemplar_w4_dequantize(q, dtype, out=None, stream=None):
     """The values of W4Rows q as an n x d tensor of ``dtype``."""
     prec = _precision(dtype)
     _w4_check(q, "q")
-    out = _out(out, (q.n, q.d), dtype, q.codes.device, stream)
+    if out is None:
+        out = _empty(stream)((q.n, q.d), dtype=dtype, device=q.codes.device)
+    elif out.dtype != dtype or out.shape != (q.n, q.d):
+        raise ValueError(f"out must be a {q.n} x {q.d} tensor of {dtype}")
     _run("exemplar_w4_dequantize", (q.codes, q.words, out), stream, q.codes.data_ptr(), q.words.data_ptr(), q.n, q.d,
          q.group, prec, out.data_ptr())
     return out
@@ -732,7 +761,7 @@ def exemplar_w4_product(x, W, bias=None, out=None, stream=None):
     if wd != d:
         raise ValueError("x and W must have the same number of coordinates")
     _bias_check(bias, f, "bias")
-    out = _out(out, (n, f), dtype, x.device, stream)
+    out = _out(out, (n, f), x, stream)
     _run("exemplar_w4_product", (x, codes, words, bias, out), stream, x.data_ptr(), n, d, prec, codes.data_ptr(),
          words.data_ptr(), f, group, _at(bias), out.data_ptr())
     return out
@@ -753,7 +782,7 @@ def exemplar_w4_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, out=Non
         raise ValueError("Wg and Wu must have x's number of coordinates, one number of rows and one group size")
     _bias_check(bg, f, "bg")
     _bias_check(bu, f, "bu")
-    out = _out(out, (n, f), dtype, x.device, stream)
+    out = _out(out, (n, f), x, stream)
     _run("exemplar_w4_glu", (x, Wg.codes, Wg.words, Wu.codes, Wu.words, bg, bu, out), stream, x.data_ptr(), n, d, prec,
          Wg.codes.data_ptr(), Wg.words.data_ptr(), Wu.codes.data_ptr(), Wu.words.data_ptr(), f, Wg.group, _at(bg), _at(bu),
          activation, out.data_ptr())

@@ -30,6 +30,7 @@ namespace exemcl {
 
 constexpr int kRowsWaves = 8;
 
+
 // Eight elements of a row of x or of 16- or 32-bit weights as operands.
 template <typename T>
 struct RowsFrag {
@@ -103,13 +104,14 @@ struct RowsArgs {
 };
 
 // GROUP 0: weights of type T; else 4-bit ones with so many to a group.  RT tiles
-// of 16 weights' rows a wavefront (GLU: of both matrices), 16 MT rows of x.
-template <typename T, int GROUP, bool GLU, int RT, int MT>
+// of 16 weights' rows a wavefront (GLU: of both matrices), 16 MT rows of x; AHEAD
+// blocks of a wavefront are loaded before the first is used.
+template <typename T, int GROUP, bool GLU, int RT, int MT, int AHEAD>
 __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a) {
     using E = typename Operand<T>::E;
     using vec = typename Mfma<E, 16>::vec_t;
     constexpr int MATS = GLU ? 2 : 1, TILES = RT * MATS;
-    constexpr int UNITS = RT * MT, PASS = UNITS < 8 / TILES ? UNITS : (8 / TILES > 0 ? 8 / TILES : 1);
+    constexpr int UNITS = RT * MT, MOST = 4 / MATS, PASS = UNITS < MOST ? UNITS : MOST;
     __shared__ f32x4 sums[kRowsWaves][PASS * MATS][64];
     const int lane = threadIdx.x & 63, lr = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -146,33 +148,52 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
         for (int m = 0; m < MT; ++m) acc[t][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     const int blocks = (int)w4_blocks(d), whole = (int)(d / kW4Block);
-    auto block = [&](int b, auto full) {
-        auto load = [&](const T *row, int j) {
-            const int k = b * kW4Block + 32 * j + 8 * g;
-            return rows_frag<T>(load8(row + (full ? k : min((int64_t)k, d - 1)), full ? 8 : (int)(d - k)));
-        };
+    // A block as it comes from memory: the weights and their words, and x (many rows
+    // of which are read when they are needed).
+    constexpr bool HOLD = MT == 1;
+    constexpr int STEPS = GROUP ? GROUP / 32 : 4, GPB = 4 / STEPS;  // instructions per group, groups per block
+    struct Block {
+        u32x4 c[GROUP ? TILES : 1], sz[GROUP ? TILES : 1][GPB];
+        typename Chunk<T>::vec w[GROUP ? 1 : TILES][4], x[4];
+    };
+    auto chunk = [&](const T *row, int b, int j, auto full) {
+        const int k = b * kW4Block + 32 * j + 8 * g;
+        return load8(row + (full ? k : min((int64_t)k, d - 1)), full ? 8 : (int)(d - k));
+    };
+    auto load = [&](Block &r, int b, auto full) {
+        if constexpr (GROUP == 0) {
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r.w[t][j] = chunk(w[t], b, j, full);
+        } else {
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                r.c[t] = codes[t][b * 64];
+#pragma unroll
+                for (int q = 0; q < GPB; ++q) r.sz[t][q] = words[t][(b * GPB + q) * 4];
+            }
+        }
+        if constexpr (HOLD)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r.x[j] = chunk(x[0], b, j, full);
+    };
+    auto use = [&](const Block &r, int b, auto full) {
+        auto x_frag = [&](int m, int j) { return rows_frag<T>(HOLD ? r.x[j] : chunk(x[m], b, j, full)); };
         if constexpr (GROUP == 0) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 RowsFrag<T> wf[TILES];
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) wf[t] = load(w[t], j);
+                for (int t = 0; t < TILES; ++t) wf[t] = rows_frag<T>(r.w[t][j]);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    const RowsFrag<T> xf = load(x[m], j);
+                    const RowsFrag<T> xf = x_frag(m, j);
 #pragma unroll
                     for (int t = 0; t < TILES; ++t) acc[t][m] = rows_mma<T>(wf[t], xf, acc[t][m]);
                 }
             }
         } else {
-            constexpr int STEPS = GROUP / 32, GPB = 4 / STEPS;  // instructions per group, groups per block
-            u32x4 c[TILES], sz[TILES][GPB];
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                c[t] = codes[t][b * 64];
-#pragma unroll
-                for (int q = 0; q < GPB; ++q) sz[t][q] = words[t][(b * GPB + q) * 4];
-            }
             vec ones;
 #pragma unroll
             for (int e = 0; e < 8; ++e) ones[e] = (E)1.0f;
@@ -185,7 +206,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
                     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int j = 0; j < STEPS; ++j) {
-                        xf[m][j] = load(x[m], q * STEPS + j);
+                        xf[m][j] = x_frag(m, q * STEPS + j);
                         s = rows_mma_whole<T>(ones, xf[m][j], s);
                     }
                     xs[m] = s[0];
@@ -194,7 +215,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
                 for (int t = 0; t < TILES; ++t) {
                     vec wf[STEPS];
 #pragma unroll
-                    for (int j = 0; j < STEPS; ++j) wf[j] = w4_operand(c[t][q * STEPS + j], E());
+                    for (int j = 0; j < STEPS; ++j) wf[j] = w4_operand(r.c[t][q * STEPS + j], E());
 #pragma unroll
                     for (int m = 0; m < MT; ++m) {
                         f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -202,7 +223,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
                         for (int j = 0; j < STEPS; ++j) p = rows_mma_whole<T>(wf[j], xf[m][j], p);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const uint32_t word = sz[t][q][i];
+                            const uint32_t word = r.sz[t][q][i];
                             acc[t][m][i] = fmaf(__uint_as_float(word & 0xffffff00u),
                                                 fmaf(-(float)(word & 0xffu), xs[m], p[i]), acc[t][m][i]);
                         }
@@ -211,8 +232,21 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
             }
         }
     };
-    for (int b = wave; b < whole; b += kRowsWaves) block(b, std::true_type());
-    if (whole < blocks && whole % kRowsWaves == wave) block(whole, std::false_type());
+    for (int b0 = wave; b0 < whole; b0 += kRowsWaves * AHEAD) {
+        Block r[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) load(r[i], min(b0 + i * kRowsWaves, whole - 1), std::true_type());
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i == 0 || b0 + i * kRowsWaves < whole) use(r[i], b0 + i * kRowsWaves, std::true_type());
+        }
+    }
+    if (whole < blocks && whole % kRowsWaves == wave) {
+        Block r;
+        load(r, whole, std::false_type());
+        use(r, whole, std::false_type());
+    }
 
     // The wavefronts' sums, PASS units of a tile and 16 rows at a time, each added
     // and finished by one wavefront.
@@ -256,13 +290,13 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
     }
 }
 
-template <typename T, int GROUP, bool GLU, int RT, int MT>
+template <typename T, int GROUP, bool GLU, int RT, int MT, int AHEAD>
 hipError_t rows_launch(RowsArgs a, hipStream_t st) {
     a.mblocks = (a.n + 16 * MT - 1) / (16 * MT);
     a.units = ((a.f + 15) / 16 + RT - 1) / RT;
     const int64_t groups = (a.units + 7) / 8;
     if (groups > (int64_t(1) << 31) / a.mblocks) return hipErrorInvalidValue;  // 2^14 rows of kFlatRow
-    hipLaunchKernelGGL((rows_kernel<T, GROUP, GLU, RT, MT>), flat_grid(groups * 8 * a.mblocks, kRowsWaves * 64),
+    hipLaunchKernelGGL((rows_kernel<T, GROUP, GLU, RT, MT, AHEAD>), flat_grid(groups * 8 * a.mblocks, kRowsWaves * 64),
                        dim3(kRowsWaves * 64), 0, st, a);
     return hipGetLastError();
 }

@@ -8,8 +8,11 @@ namespace exemcl {
 
 template <typename T, int GROUP, bool GLU>
 hipError_t w4_sized(const RowsArgs &r, hipStream_t st) {
-    if (r.n <= 16) return rows_launch<T, GROUP, GLU, 1, 1>(r, st);
-    if (r.n <= 64) return rows_launch<T, GROUP, GLU, GLU ? 1 : 2, 4>(r, st);
+    // Two blocks ahead pay where a block is few registers (us, one row, bf16, 1 / 2 / 4
+    // ahead: 8192 x 4096 by groups of 128 8.8 / 7.8 / 8.2, 1536 x 8192 by 32 4.6 / 5.0 /
+    // 8.0); 16 wavefronts to a workgroup spill.
+    if (r.n <= 16) return rows_launch<T, GROUP, GLU, 1, 1, (GROUP >= 64 ? 2 : 1)>(r, st);
+    if (r.n <= 64) return rows_launch<T, GROUP, GLU, GLU ? 1 : 2, 4, 1>(r, st);
     return w4_tile_launch<T, GROUP, GLU>(r, st);
 }
 
