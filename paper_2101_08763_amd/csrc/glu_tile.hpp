@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "glu_device.hpp"
 #include "mfma_kernels.hpp"
@@ -37,18 +38,26 @@ struct DenseLaunch {
     const float *bg, *bu;
     int act;
     void *C, *C2, *g, *u;
+    int splits;     // of the sum, over workgroups; partial: splits x pairs x M x N sums
+    float *partial;
 };
 
-template <int AF>
+// Tiles: PM x PN wavefronts, quarters of 16 AF x 32 results; BUFFERS stages in LDS.
+template <int AF_, int PM_, int PN_, int BUFFERS_>
 struct DensePlan {
-    static constexpr int WAVES = 8, THREADS = WAVES * 64, BK = 64;
-    static constexpr int BM = 64 * AF, BN = 256;
+    static constexpr int AF = AF_, PM = PM_, PN = PN_, BUFFERS = BUFFERS_;
+    static constexpr int WAVES = PM * PN, THREADS = WAVES * 64, BK = 64;
+    static constexpr int BM = PM * 32 * AF, BN = PN * 64;
     static constexpr int A_ROWS = BM / 2, B_ROWS = BN / 2;  // of a region
     static constexpr int A_REGION = A_ROWS * BK * 2, B_REGION = B_ROWS * BK * 2;
     static constexpr int A_LOADS = A_REGION / (THREADS * 16), B_LOADS = B_REGION / (THREADS * 16);
-    static constexpr int STAGE = 2 * (A_REGION + B_REGION), LDS = 2 * STAGE;
+    static constexpr int LOADS = 2 * (A_LOADS + B_LOADS);  // of a thread and stage
+    static constexpr int STAGE = 2 * (A_REGION + B_REGION), LDS = BUFFERS * STAGE;
+    static constexpr bool PHASED = WAVES == 8;  // two groups of wavefronts half a phase apart
     static_assert(A_LOADS >= 1 && LDS <= kLdsBytes, "geometry");
 };
+using LargeTile = DensePlan<4, 2, 4, 2>;  // 256 x 256
+using SmallTile = DensePlan<1, 2, 2, 3>;  // 64 x 128
 
 // Places in a region.  ALONG: a row of 8 chunks of 16 bytes (8 steps of t) per
 // row of the operand; chunk c of row p is at c ^ swap(p), so that 16 rows read at
@@ -57,7 +66,9 @@ struct DensePlan {
 __device__ __forceinline__ int along_swap(int p) { return p >> 1 & 7; }
 template <bool FIRST, int CHUNKS>
 __device__ __forceinline__ int across_swap(int t) {
-    if constexpr (FIRST) return (t & 1) | (t >> 1 & 1) << 2 | (t >> 3 & 1) << 3;
+    if constexpr (FIRST && CHUNKS == 16) return (t & 1) | (t >> 1 & 1) << 2 | (t >> 3 & 1) << 3;
+    if constexpr (FIRST) return (t >> 3 & 1) | (t >> 1 & 1) << 2;
+    if constexpr (CHUNKS == 4) return (t >> 3 & 1) << 1;
     if constexpr (CHUNKS == 8) return (t >> 1 & 1) << 1 | (t >> 3 & 1) << 2;
     return (t & 3) << 1 | (t >> 3 & 1) << 3;
 }
@@ -97,22 +108,37 @@ __device__ __forceinline__ void read_across(uint32_t at0, uint32_t at1, u32x2t (
         : "memory");
 }
 
-template <typename T, int LA, int LB, int EPI, int AF>
-__global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
-    using P = DensePlan<AF>;
+// The same for one fragment.
+template <int ROW>
+__device__ __forceinline__ void read_across(uint32_t at, u32x2t (&v)[2][2]) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %4\n\t"
+        "ds_read_b64_tr_b16 %1, %4 offset:%5\n\t"
+        "ds_read_b64_tr_b16 %2, %4 offset:%6\n\t"
+        "ds_read_b64_tr_b16 %3, %4 offset:%7\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0][0]), "=&v"(v[0][1]), "=&v"(v[1][0]), "=&v"(v[1][1])
+        : "v"(at), "n"(4 * ROW), "n"(32 * ROW), "n"(36 * ROW)
+        : "memory");
+}
+
+template <typename T, int LA, int LB, int EPI, typename P>
+__global__ __launch_bounds__(P::THREADS, 2) void dense_kernel(const DenseLaunch a) {
+    constexpr int AF = P::AF;
     using E = typename Operand<T>::E;
     using M = Mfma<E, 16>;
     using vec = typename M::vec_t;
     constexpr int PRODUCTS = Operand<T>::PRODUCTS, BK = P::BK;
     extern __shared__ __align__(16) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, g = lane >> 4;
-    const int wave = uniform(tid >> 6), wm = wave >> 2, wn = wave & 3;
+    const int wave = uniform(tid >> 6), wm = wave / P::PN, wn = wave % P::PN;
 
     // Workgroups b, b + 8, b + 16, ... share an XCD and its L2: they take
     // consecutive tiles, up to 8 of one row of tiles side by side.
-    const int mblocks = a.mblocks * a.pairs, units = mblocks * a.nblocks, per = (units + 7) / 8;
-    const int wg = (int)flat_block(), pos = wg >> 3, un = (wg & 7) * per + pos;
-    if (pos >= per || un >= units) return;
+    const int mblocks = a.mblocks * a.pairs, tiles = mblocks * a.nblocks, units = tiles * a.splits, per = (units + 7) / 8;
+    const int wg = (int)flat_block(), pos = wg >> 3, all = (wg & 7) * per + pos;
+    if (pos >= per || all >= units) return;
+    const int split = uniform((uint32_t)all / (uint32_t)tiles), un = all - split * tiles;
     const int strip = uniform((uint32_t)un / (uint32_t)(mblocks * 8)), width = min(8, a.nblocks - strip * 8);
     const int in = un - strip * mblocks * 8;
     const int mt = uniform((uint32_t)in / (uint32_t)width), nt = strip * 8 + in - mt * width;
@@ -124,10 +150,13 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
 
     // Stages: for every pair of a matrix and a product of parts, K in steps of 64.
     // The products of small parts come first, while the sums are small.
-    const int pairs = PRODUCTS * a.matrices, stages = (int)((K + BK - 1) / BK) * pairs;
+    // A split takes a part of them.
+    const int pairs = PRODUCTS * a.matrices, ksteps = (int)((K + BK - 1) / BK);
+    const int each = (int)((uint32_t)(ksteps * pairs + a.splits - 1) / (uint32_t)a.splits);
+    const int first = split * each, stages = max(0, min(each, ksteps * pairs - first));
     const E *at = nullptr, *bt = nullptr, *bt2 = nullptr;  // the operands of the stage to issue next
-    int is_pair = 0;
-    uint32_t is_k = 0;
+    int is_pair = uniform((uint32_t)first / (uint32_t)ksteps);
+    uint32_t is_k = (uint32_t)(first - is_pair * ksteps) * BK;
     auto pair = [&]() {
         const int mat = is_pair / PRODUCTS, p = PRODUCTS - 1 - (is_pair - mat * PRODUCTS);
         const int64_t pa = PRODUCTS > 1 ? part_a(p) * a.plane_a : 0, pb = PRODUCTS > 1 ? part_b(p) * a.plane_b : 0;
@@ -135,7 +164,9 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
         bt = uniform((const E *)(mat ? a.B2 : a.B) + pb + (LB == ALONG ? (int64_t)n0 * ldb : n0));
         if constexpr (EPI == GLU) bt2 = uniform((const E *)a.B2 + pb + (int64_t)n0 * ldb);
     };
-    pair();
+    if (is_pair < pairs) pair();
+    if constexpr (LA == ACROSS) at += (int64_t)is_k * lda;
+    if constexpr (LB == ACROSS) bt += (int64_t)is_k * ldb;
 
     // What a thread copies of a region: a chunk of 16 bytes per load.  `off` is
     // its place in the window of the first half, `t` its first step of t.
@@ -167,15 +198,16 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
             b_off[i] = (uint32_t)(row * ldb + c * 8) * 2;
             b_t[i] = c * 8;
         } else {
-            const int t = q / 16, e = ((q % 16) ^ across_swap<true, 16>(t)) * 8;
+            constexpr int CHUNKS = P::B_ROWS / 8;
+            const int t = q / CHUNKS, e = ((q % CHUNKS) ^ across_swap<true, CHUNKS>(t)) * 8;
             b_off[i] = (uint32_t)(t * ldb + e / 32 * APART + e % 32) * 2;
             b_t[i] = t;
         }
     }
-    // Copies of half h of the stage's A or B into buffer `buf`.  ALONG: the window
+    // Copies of half h of the stage's A or B into the buffer at `to`.  ALONG: the window
     // is the tile's rows, and a chunk past K is dead; ACROSS: it is the steps of t
     // that are left.  Past the last stage the window is empty.
-    auto issue_a = [&](int h, int buf) {
+    auto issue_a = [&](int h, int to) {
         uint32_t bytes = LA == ALONG ? (uint32_t)mrows * (uint32_t)lda * 2 : (min((uint32_t)BK, K - is_k) * (uint32_t)lda - (uint32_t)m0) * 2;
         if (is_pair >= pairs) bytes = 0;
         const auto win = window_rsrc(at, bytes);
@@ -183,10 +215,10 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
         for (int i = 0; i < P::A_LOADS; ++i) {
             uint32_t off = a_off[i] + (uint32_t)(LA == ALONG ? h * 16 * AF * lda * 2 + is_k * 2 : h * 16 * AF * 2);
             if constexpr (LA == ALONG) off = is_k + a_t[i] < K ? off : kDeadOffset;
-            window_to_lds16(win, smem + buf * P::STAGE + h * P::A_REGION + (wave * P::A_LOADS + i) * 1024, off);
+            window_to_lds16(win, smem + to + h * P::A_REGION + (wave * P::A_LOADS + i) * 1024, off);
         }
     };
-    auto issue_b = [&](int h, int buf) {
+    auto issue_b = [&](int h, int to) {
         uint32_t bytes = LB == ALONG ? (uint32_t)nrows * (uint32_t)ldb * 2 : (min((uint32_t)BK, K - is_k) * (uint32_t)ldb - (uint32_t)n0) * 2;
         if (is_pair >= pairs) bytes = 0;
         const auto win = window_rsrc(EPI == GLU && h ? bt2 : bt, bytes);
@@ -195,7 +227,7 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
         for (int i = 0; i < P::B_LOADS; ++i) {
             uint32_t off = b_off[i] + (uint32_t)(LB == ALONG ? half * 32 * ldb * 2 + is_k * 2 : half * 32 * 2);
             if constexpr (LB == ALONG) off = is_k + b_t[i] < K ? off : kDeadOffset;
-            window_to_lds16(win, smem + buf * P::STAGE + 2 * P::A_REGION + h * P::B_REGION + (wave * P::B_LOADS + i) * 1024, off);
+            window_to_lds16(win, smem + to + 2 * P::A_REGION + h * P::B_REGION + (wave * P::B_LOADS + i) * 1024, off);
         }
     };
     auto issued = [&]() {
@@ -211,9 +243,8 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
     // Operands of one half from LDS, fragments of 16 rows x 32 steps.
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
     auto join = [](u32x2t lo, u32x2t hi) { return __builtin_bit_cast(vec, u32x4{lo[0], lo[1], hi[0], hi[1]}); };
-    vec av[AF][2], bv[3][2][2];  // [fragment][32 steps]; B's second half, and the first one's of both buffers
-    auto read_a = [&](int h, int buf) {
-        const int region = buf * P::STAGE + h * P::A_REGION;
+    auto read_a = [&](int h, int from, vec(&av)[AF][2]) {  // [fragment][32 steps]
+        const int region = from + h * P::A_REGION;
         if constexpr (LA == ALONG) {
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks)
@@ -225,25 +256,30 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
         } else {
             constexpr int CHUNKS = P::A_ROWS / 8;
             const int t = 8 * g + (lr >> 2);
+            auto place = [&](int w) {
+                const int c = wm * 2 * AF + w * 2 + (lr >> 1 & 1);
+                return lds + region + t * CHUNKS * 16 + (c ^ across_swap<false, CHUNKS>(t)) * 16 + (lr & 1) * 8;
+            };
+            if constexpr (AF == 1) {
+                u32x2t v[2][2];
+                read_across<CHUNKS * 16>(place(0), v);
 #pragma unroll
-            for (int w = 0; w < AF; w += 2) {
-                uint32_t from[2];
+                for (int ks = 0; ks < 2; ++ks) av[0][ks] = join(v[ks][0], v[ks][1]);
+            } else {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int c = wm * 2 * AF + (w + e) * 2 + (lr >> 1 & 1);
-                    from[e] = lds + region + t * CHUNKS * 16 + (c ^ across_swap<false, CHUNKS>(t)) * 16 + (lr & 1) * 8;
+                for (int w = 0; w < AF; w += 2) {
+                    u32x2t v[2][2][2];
+                    read_across<CHUNKS * 16>(place(w), place(w + 1), v);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int ks = 0; ks < 2; ++ks) av[w + e][ks] = join(v[e][ks][0], v[e][ks][1]);
                 }
-                u32x2t v[2][2][2];
-                read_across<CHUNKS * 16>(from[0], from[1], v);
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks) av[w + e][ks] = join(v[e][ks][0], v[e][ks][1]);
             }
         }
     };
-    auto read_b = [&](int h, int buf, vec(&to)[2][2]) {
-        const int region = buf * P::STAGE + 2 * P::A_REGION + h * P::B_REGION;
+    auto read_b = [&](int h, int from, vec(&to)[2][2]) {
+        const int region = from + 2 * P::A_REGION + h * P::B_REGION;
         if constexpr (LB == ALONG) {
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks)
@@ -253,10 +289,11 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
                     to[j][ks] = *reinterpret_cast<const vec *>(smem + region + p * 128 + ((ks * 4 + g) ^ along_swap(lr)) * 16);
                 }
         } else {
+            constexpr int CHUNKS = P::B_ROWS / 8;
             const int t = 8 * g + (lr >> 2), c = wn * 4 + (lr & 3);
-            const uint32_t from = lds + region + t * 256 + (c ^ across_swap<true, 16>(t)) * 16 + (lr & 1) * 8;
+            const uint32_t at = lds + region + t * CHUNKS * 16 + (c ^ across_swap<true, CHUNKS>(t)) * 16 + (lr & 1) * 8;
             u32x2t v[2][2][2];
-            read_across<256>(from, from ^ 8, v);
+            read_across<CHUNKS * 16>(at, at ^ 8, v);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -273,70 +310,111 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) acc[ha][w][hb][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // A phase: reads for one quarter of the tile and copies for the stage after
-    // next, then the quarter's instructions.  The wavefronts 0 .. 3 are half a phase
-    // ahead of 4 .. 7, with which they share the SIMDs: while one reads, the other
-    // multiplies.  What is read in a phase has been waited for, by every wavefront,
-    // in the one before it; the copies go to the region that was read there.
-    auto ready = [&]() {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * (P::A_LOADS + P::B_LOADS)) : "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto multiply = [&](int ha, int hb, const vec(&b)[2][2]) {
-        __builtin_amdgcn_s_setprio(1);
+    auto multiply = [&](int ha, int hb, const vec(&av)[AF][2], const vec(&b)[2][2]) {
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int w = 0; w < AF; ++w)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) acc[ha][w][hb][j] = M::mma(b[j][ks], av[w][ks], 0, acc[ha][w][hb][j]);
-        __builtin_amdgcn_s_setprio(0);
+    };
+    auto issue = [&](int to) {
+        issue_b(0, to);
+        issue_a(0, to);
+        issue_b(1, to);
+        issue_a(1, to);
+        issued();
+    };
+    auto next = [](int at) { return at == (P::BUFFERS - 1) * P::STAGE ? 0 : at + P::STAGE; };
+    if constexpr (P::PHASED) {
+        // A phase: reads for one quarter of the tile and copies for the stage that
+        // comes into this buffer next, then the quarter's instructions.  The
+        // wavefronts 0 .. 3 are half a phase ahead of 4 .. 7, with which they share the
+        // SIMDs: while one reads, the other multiplies.  What is read in a phase has
+        // been waited for, by every wavefront, in the one before it; the copies go to
+        // the region that was read there.
+        vec av[AF][2], bv[3][2][2];  // B's second half, and the first one's of two stages
+        // (two regions of the stage before, and whole stages)
+        constexpr int FLYING = P::LOADS / 2 + (P::BUFFERS - 1) * P::LOADS;
+        auto ready = [&]() {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLYING) : "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto quarter = [&](int ha, int hb, const vec(&b)[2][2]) {
+            __builtin_amdgcn_s_setprio(1);
+            multiply(ha, hb, av, b);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto stage = [&](auto parity, int at) {
+            constexpr int own = 1 + decltype(parity)::value, others = 3 - own;
+            read_a(0, at, av);
+            issue_b(0, at);
+            ready();
+            quarter(0, 0, bv[own]);
+            read_b(1, at, bv[0]);
+            issue_a(0, at);
+            ready();
+            quarter(0, 1, bv[0]);
+            read_a(1, at, av);
+            issue_b(1, at);
+            ready();
+            quarter(1, 1, bv[0]);
+            read_b(0, next(at), bv[others]);
+            issue_a(1, at);
+            issued();
+            ready();
+            quarter(1, 0, bv[own]);
+        };
+#pragma unroll
+        for (int buf = 0; buf < P::BUFFERS; ++buf) issue(buf * P::STAGE);
+        ready();
+        read_b(0, 0, bv[1]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_barrier();
+        if (wave >= 4) __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-    };
-    auto stage = [&](auto parity) {
-        constexpr int buf = decltype(parity)::value;
-        read_a(0, buf);
-        issue_b(0, buf);
-        ready();
-        multiply(0, 0, bv[1 + buf]);
-        read_b(1, buf, bv[0]);
-        issue_a(0, buf);
-        ready();
-        multiply(0, 1, bv[0]);
-        read_a(1, buf);
-        issue_b(1, buf);
-        ready();
-        multiply(1, 1, bv[0]);
-        read_b(0, 1 - buf, bv[2 - buf]);
-        issue_a(1, buf);
-        issued();
-        ready();
-        multiply(1, 0, bv[1 + buf]);
-    };
+        int at = 0;
+        for (int st = 0; st < stages; st += 2) {
+            stage(std::integral_constant<int, 0>(), at);
+            at = next(at);
+            if (st + 1 < stages) {
+                stage(std::integral_constant<int, 1>(), at);
+                at = next(at);
+            }
+        }
+        if (wave < 4) __builtin_amdgcn_s_barrier();
+    } else {
+        // Two such workgroups share a CU, and each covers the other's waits.
 #pragma unroll
-    for (int buf = 0; buf < 2; ++buf) {
-        issue_b(0, buf);
-        issue_a(0, buf);
-        issue_b(1, buf);
-        issue_a(1, buf);
-        issued();
+        for (int buf = 0; buf < P::BUFFERS - 1; ++buf) issue(buf * P::STAGE);
+        int at = 0, to = (P::BUFFERS - 1) * P::STAGE;
+        for (int st = 0; st < stages; ++st) {
+            // (__syncthreads would wait for all copies)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((P::BUFFERS - 2) * P::LOADS) : "memory");  // stage st
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();  // everyone's, and the one before it has been read
+            __builtin_amdgcn_sched_barrier(0);
+            issue(to);
+            vec av[2][AF][2], bv[2][2][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                read_b(h, at, bv[h]);
+                read_a(h, at, av[h]);
+            }
+#pragma unroll
+            for (int ha = 0; ha < 2; ++ha)
+#pragma unroll
+                for (int hb = 0; hb < 2; ++hb) multiply(ha, hb, av[ha], bv[hb]);
+            to = at;
+            at = next(at);
+        }
     }
-    ready();
-    read_b(0, 0, bv[1]);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_barrier();
-    if (wave >= 4) __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    for (int st = 0; st < stages; st += 2) {
-        stage(std::integral_constant<int, 0>());
-        if (st + 1 < stages) stage(std::integral_constant<int, 1>());
-    }
-    if (wave < 4) __builtin_amdgcn_s_barrier();
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the last copies
 
     // Row w * 16 + lr of a quarter, and its columns 8 g .. 8 g + 7: fragment g % 2
@@ -380,29 +458,65 @@ __global__ __launch_bounds__(512, 2) void dense_kernel(const DenseLaunch a) {
                 }
         });
     } else {
-        T *C = (T *)(other ? a.C2 : a.C);
+        auto store_to = [&](auto *C) {
 #pragma unroll
-        for (int ha = 0; ha < 2; ++ha)
+            for (int ha = 0; ha < 2; ++ha)
 #pragma unroll
-            for (int w = 0; w < AF; ++w) {
-                const int64_t row = m0 + wm * 32 * AF + ha * 16 * AF + w * 16 + lr;
-                if (row >= a.M) continue;
+                for (int w = 0; w < AF; ++w) {
+                    const int64_t row = m0 + wm * 32 * AF + ha * 16 * AF + w * 16 + lr;
+                    if (row >= a.M) continue;
 #pragma unroll
-                for (int hb = 0; hb < 2; ++hb) {
-                    const int64_t col = n0 + wn * 64 + hb * 32 + 8 * g;
-                    const int have = (int)max((int64_t)0, min((int64_t)8, a.N - col));
-                    float v[8];
-                    eight(acc[ha][w][hb], v);
-                    store8(C + row * a.N + col, have, v);
+                    for (int hb = 0; hb < 2; ++hb) {
+                        const int64_t col = n0 + wn * 64 + hb * 32 + 8 * g;
+                        const int have = (int)max((int64_t)0, min((int64_t)8, a.N - col));
+                        float v[8];
+                        eight(acc[ha][w][hb], v);
+                        store8(C + row * a.N + col, have, v);
+                    }
                 }
-            }
+        };
+        if (a.splits == 1)
+            store_to((T *)(other ? a.C2 : a.C));
+        else
+            store_to(a.partial + ((int64_t)split * a.pairs + other) * a.M * a.N);
     }
 }
 
-template <typename T, int LA, int LB, int EPI, int AF>
+// out = the splits' sums, added in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void dense_join_kernel(const float *__restrict__ partial, int splits, int64_t count,
+                                                         int64_t of_one, T *__restrict__ C, T *__restrict__ C2) {
+    const int64_t at = (flat_block() * 256 + threadIdx.x) * 4;
+    if (at >= count) return;
+    const int have = (int)min((int64_t)4, count - at);
+    typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+    float s[4] = {};
+    for (int i = 0; i < splits; ++i) {
+        const float *p = partial + i * count + at;
+        if (have == 4) {
+            const vec v = *reinterpret_cast<const vec *>(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += v[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < have) s[e] += p[e];
+        }
+    }
+    if (at + have <= of_one) {
+        store4(C + at, have, s);
+    } else if (at >= of_one) {
+        store4(C2 + (at - of_one), have, s);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < have) (at + e < of_one ? C[at + e] : C2[at + e - of_one]) = (T)s[e];
+    }
+}
+
+template <typename T, int LA, int LB, int EPI, typename P>
 hipError_t dense_launch(DenseLaunch a, hipStream_t st) {
-    using P = DensePlan<AF>;
-    auto kern = dense_kernel<T, LA, LB, EPI, AF>;
+    auto kern = dense_kernel<T, LA, LB, EPI, P>;
     static std::atomic<bool> ready[kMaxDevices];  // the attribute holds for one device
     const int dev = current_device();
     if (dev < 0) return hipErrorInvalidDevice;
@@ -413,20 +527,55 @@ hipError_t dense_launch(DenseLaunch a, hipStream_t st) {
     }
     constexpr int BN = EPI == GLU ? P::BN / 2 : P::BN;
     const int64_t mb = (a.M + P::BM - 1) / P::BM, nb = (a.N + BN - 1) / BN;
-    if (mb * a.pairs > (int64_t(1) << 30) / nb) return hipErrorInvalidValue;
+    if (mb * a.pairs * a.splits > (int64_t(1) << 30) / nb) return hipErrorInvalidValue;
     a.mblocks = (int)mb;
     a.nblocks = (int)nb;
-    hipLaunchKernelGGL(kern, flat_grid((mb * a.pairs * nb + 7) / 8 * 8, P::THREADS), dim3(P::THREADS), P::LDS, st, a);
+    hipLaunchKernelGGL(kern, flat_grid((mb * a.pairs * a.splits * nb + 7) / 8 * 8, P::THREADS), dim3(P::THREADS), P::LDS, st, a);
     return hipGetLastError();
 }
 
-// The kernel for a size: 256 x 256 tiles.
+// Tiles and splits for a product of M x N (pairs times), `stages` steps long.
+struct DenseChoice {
+    bool large;
+    int splits;
+};
+inline DenseChoice dense_choice(int64_t M, int64_t N, int64_t pairs, int64_t stages, bool glu, bool may_split) {
+    const double cus = (double)std::max<int64_t>(1, device_cu_count());
+    const int64_t half = glu ? 2 : 1;
+    DenseChoice best{false, 1};
+    double least = 0.0;
+    for (const bool large : {false, true}) {
+        const int64_t bm = large ? LargeTile::BM : SmallTile::BM, bn = (large ? LargeTile::BN : SmallTile::BN) / half;
+        const double tiles = (double)(((M + bm - 1) / bm) * ((N + bn - 1) / bn) * pairs);
+        for (int64_t s = 1; s <= 32 && s <= stages; s = s < 4 ? s + 1 : s + s / 4) {
+            if (s > 1 && (!may_split || (double)s * (double)(pairs * M * N) > 2.5e8)) break;
+            const double each = (double)((stages + s - 1) / s);
+            double t = std::max(1.0, std::ceil(tiles * (double)s / cus)) * (large ? 1.4 * each + 6.0 : 0.45 * each + 3.0);
+            if (s > 1) t += 4.0 + 2.2e-6 * (double)(s * pairs * M * N);
+            if (least == 0.0 || t < least) least = t, best = {large, (int)s};
+        }
+    }
+    return best;
+}
+
 template <typename T, int LA, int LB, int EPI>
-hipError_t dense_run(const DenseLaunch &a, hipStream_t st) {
-    const int64_t cus = std::max<int64_t>(1, device_cu_count());
-    const int64_t bn = EPI == GLU ? 128 : 256;
-    if (((a.M + 255) / 256) * a.pairs * ((a.N + bn - 1) / bn) >= cus) return dense_launch<T, LA, LB, EPI, 4>(a, st);
-    return dense_launch<T, LA, LB, EPI, 2>(a, st);
+hipError_t dense_run(DenseLaunch a, hipStream_t st) {
+    const int64_t stages = (a.K + 63) / 64 * Operand<T>::PRODUCTS * a.matrices;
+    const DenseChoice c = dense_choice(a.M, a.N, a.pairs, stages, EPI == GLU, a.partial != nullptr);
+    a.splits = c.splits;
+    const hipError_t e = c.large ? dense_launch<T, LA, LB, EPI, LargeTile>(a, st) : dense_launch<T, LA, LB, EPI, SmallTile>(a, st);
+    if (e != hipSuccess || c.splits == 1) return e;
+    const int64_t of_one = a.M * a.N, count = of_one * a.pairs;
+    hipLaunchKernelGGL(dense_join_kernel<T>, flat_grid((count + 1023) / 1024, 256), dim3(256), 0, st, a.partial, c.splits,
+                       count, of_one, (T *)a.C, (T *)a.C2);
+    return hipGetLastError();
+}
+
+// Bytes of the splits' sums.
+template <typename T>
+int64_t dense_partial_bytes(int64_t M, int64_t N, int64_t K, int64_t pairs, int64_t matrices) {
+    const DenseChoice c = dense_choice(M, N, pairs, (K + 63) / 64 * Operand<T>::PRODUCTS * matrices, false, true);
+    return c.splits == 1 ? 0 : c.splits * pairs * M * N * 4;
 }
 
 inline DenseLaunch dense_args(const DenseArgs &a) {
@@ -437,6 +586,7 @@ inline DenseLaunch dense_args(const DenseArgs &a) {
     l.matrices = 1, l.pairs = 1;
     l.bg = a.bg, l.bu = a.bu, l.act = a.act;
     l.C = a.C, l.C2 = a.C2, l.g = a.g, l.u = a.u;
+    l.splits = 1, l.partial = a.partial;
     return l;
 }
 

@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <mutex>
 #include <thread>
 #include <utility>
@@ -936,10 +937,15 @@ struct StagedRows {
         if (copied) at = t->take(n * dense_ld(d) * dense_planes(prec) * 2);
     }
     const void *ptr(const Pieces &t) const { return copied ? t.base + at : src; }
-    hipError_t stage(int prec, const Pieces &t, hipStream_t st) const {
-        return copied ? launch_dense_stage(prec, src, n, d, t.base + at, st) : hipSuccess;
-    }
 };
+
+hipError_t stage_rows(int prec, const Pieces &t, std::initializer_list<const StagedRows *> rows, hipStream_t st) {
+    DenseStageJob jobs[3];
+    int count = 0;
+    for (const StagedRows *r : rows)
+        if (r->copied) jobs[count++] = {r->src, r->n, r->d, t.base + r->at};
+    return count ? launch_dense_stage(prec, jobs, count, st) : hipSuccess;
+}
 
 int run_glu(const GluArgs &a, int prec, hipStream_t st) {
     if (glu_takes_rows(prec, a.n, a.d, a.f)) return status_of(launch_glu_rows(prec, a, st));
@@ -951,12 +957,11 @@ int run_glu(const GluArgs &a, int prec, hipStream_t st) {
         if (rc) return rc;
         t.base = (char *)ws.ptr;
     }
-    for (const StagedRows *s : {&x, &wg, &wu})
-        if (s->stage(prec, t, st) != hipSuccess) return EXEMCL_EDEVICE;
+    if (stage_rows(prec, t, {&x, &wg, &wu}, st) != hipSuccess) return EXEMCL_EDEVICE;
     const int64_t ld = dense_ld(a.d);
     // (the two weights' planes are equally far apart)
     const DenseArgs p{{x.ptr(t), nullptr, ld, a.n * ld}, {wg.ptr(t), wu.ptr(t), ld, a.f * ld}, a.n, a.f, a.d,
-                      a.bg, a.bu, a.act, a.h, nullptr, a.g, a.u};
+                      a.bg, a.bu, a.act, a.h, nullptr, a.g, a.u, nullptr};
     return status_of(launch_glu_forward(prec, p, st));
 }
 
@@ -981,23 +986,27 @@ int run_glu_grad(const GluGradArgs &a, int prec, hipStream_t st) {
         wg = StagedRows(prec, a.wg, a.f, a.d, &t);
         wu = StagedRows(prec, a.wu, a.f, a.d, &t);
     }
+    // (one after the other on the stream: they share their partial sums' memory)
+    const int64_t partial_bytes = std::max(a.dx ? glu_dx_partial(prec, a.n, a.d, a.f) : 0,
+                                           dw ? glu_dw_partial(prec, a.f, a.d, a.n, a.dwg && a.dwu ? 2 : 1) : 0);
+    const int64_t partial_at = t.take(partial_bytes);
     Scratch ws;
     const int rc = alloc_uncaptured(&ws, t.bytes, workspace_limit(), st);
     if (rc) return rc;
     t.base = (char *)ws.ptr;
-    for (const StagedRows *s : {&x, &wg, &wu})
-        if (s->stage(prec, t, st) != hipSuccess) return EXEMCL_EDEVICE;
+    float *partial = partial_bytes ? (float *)(t.base + partial_at) : nullptr;
+    if (stage_rows(prec, t, {&x, &wg, &wu}, st) != hipSuccess) return EXEMCL_EDEVICE;
     float *sum = db ? (float *)(t.base + sums) : nullptr;
     const GluPointArgs p{a.dh, a.g, a.u, a.n, a.f, a.act, t.base + dg, t.base + du, parts, sum};
     hipError_t e = launch_glu_point(prec, p, st);
     if (e == hipSuccess && a.dx) {
         const DenseArgs q{{t.base + dg, t.base + du, ldf, a.n * ldf}, {wg.ptr(t), wu.ptr(t), ldd, a.f * ldd},
-                          a.n, a.d, a.f, nullptr, nullptr, 0, a.dx, nullptr, nullptr, nullptr};
+                          a.n, a.d, a.f, nullptr, nullptr, 0, a.dx, nullptr, nullptr, nullptr, partial};
         e = launch_glu_dx(prec, q, st);
     }
     if (e == hipSuccess && dw) {
         const DenseArgs q{{t.base + dg, t.base + du, ldf, a.n * ldf}, {x.ptr(t), nullptr, ldd, a.n * ldd},
-                          a.f, a.d, a.n, nullptr, nullptr, 0, a.dwg, a.dwu, nullptr, nullptr};
+                          a.f, a.d, a.n, nullptr, nullptr, 0, a.dwg, a.dwu, nullptr, nullptr, partial};
         e = launch_glu_dw(prec, q, st);
     }
     if (e == hipSuccess && a.dbg) e = launch_column_sum(sum, parts, a.f, a.dbg, st);

@@ -328,19 +328,28 @@ struct DenseArgs {
     const float *bg, *bu;
     int act;
     void *C, *C2, *g, *u;
+    float *partial;  // glu_dx_partial or glu_dw_partial bytes (0: may be null)
 };
 int64_t dense_ld(int64_t d);
 int dense_planes(int prec);
 // Whether rows of d elements at p are an operand as they are.
 bool dense_in_place(int prec, const void *p, int64_t d);
-// Rows of d elements as an operand (rows x dense_ld(d) elements a plane).
-hipError_t launch_dense_stage(int prec, const void *src, int64_t n, int64_t d, void *dst, hipStream_t st);
+// Rows of d elements as operands (rows x dense_ld(d) elements a plane), up to three
+// arrays at once.
+struct DenseStageJob {
+    const void *src;
+    int64_t n, d;
+    void *dst;
+};
+hipError_t launch_dense_stage(int prec, const DenseStageJob *jobs, int count, hipStream_t st);
 // h (C), g and u of n rows: A = x, B = Wg and Wu.
 hipError_t launch_glu_forward(int prec, const DenseArgs &a, hipStream_t st);
 // C = A B + A2 B2: M x K times K x N.
 hipError_t launch_glu_dx(int prec, const DenseArgs &a, hipStream_t st);
+int64_t glu_dx_partial(int prec, int64_t M, int64_t N, int64_t K);
 // C = A' B, C2 = A2' B (each nullable): A is K x M, B K x N.
 hipError_t launch_glu_dw(int prec, const DenseArgs &a, hipStream_t st);
+int64_t glu_dw_partial(int prec, int64_t M, int64_t N, int64_t K, int pairs);
 
 // dg = dh u a'(g) and du = dh a(g) as operands, and the sums of their columns over
 // the rows of each part: sums is 2 x parts x f (nullable).

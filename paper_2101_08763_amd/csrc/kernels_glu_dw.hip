@@ -13,4 +13,8 @@ hipError_t launch_glu_dw(int prec, const DenseArgs &a, hipStream_t st) {
     return dense_run<__bf16, ACROSS, ACROSS, STORE>(l, st);
 }
 
+int64_t glu_dw_partial(int prec, int64_t M, int64_t N, int64_t K, int pairs) {
+    return prec == P_FP32 ? dense_partial_bytes<float>(M, N, K, pairs, 1) : dense_partial_bytes<_Float16>(M, N, K, pairs, 1);
+}
+
 }  // namespace exemcl

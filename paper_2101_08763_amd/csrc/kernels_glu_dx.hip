@@ -11,4 +11,8 @@ hipError_t launch_glu_dx(int prec, const DenseArgs &a, hipStream_t st) {
     return dense_run<__bf16, ALONG, ACROSS, STORE>(l, st);
 }
 
+int64_t glu_dx_partial(int prec, int64_t M, int64_t N, int64_t K) {
+    return prec == P_FP32 ? dense_partial_bytes<float>(M, N, K, 1, 2) : dense_partial_bytes<_Float16>(M, N, K, 1, 2);
+}
+
 }  // namespace exemcl

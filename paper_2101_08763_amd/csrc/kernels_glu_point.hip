@@ -33,20 +33,28 @@ __device__ __forceinline__ void store_operand(typename Operand<T>::E *p, int64_t
     }
 }
 
-// T: float, or uint16_t for either 16-bit type.
+// Rows as operands; T: float, or uint16_t for either 16-bit type.
+struct StageJobs {
+    DenseStageJob job[3];
+    int64_t blocks[3];  // workgroups up to and with each
+};
 template <typename T>
-__global__ __launch_bounds__(256) void dense_stage_kernel(const T *__restrict__ src, int64_t n, int64_t d, int64_t ld,
-                                                          void *__restrict__ dst) {
-    const int64_t i = flat_block() * 256 + threadIdx.x, per = ld / 8, row = i / per, c = i - row * per;
-    if (row >= n) return;
-    const int have = (int)min((int64_t)8, d - c * 8);
+__global__ __launch_bounds__(256) void dense_stage_kernel(const StageJobs jobs) {
+    int64_t b = flat_block();
+    const int which = b < jobs.blocks[0] ? 0 : b < jobs.blocks[1] ? 1 : 2;
+    if (which) b -= jobs.blocks[which - 1];
+    const DenseStageJob j = jobs.job[which];
+    const int64_t ld = (j.d + 7) / 8 * 8, per = ld / 8, i = b * 256 + threadIdx.x, row = i / per, c = i - row * per;
+    if (row >= j.n) return;
+    const T *src = (const T *)j.src + row * j.d + c * 8;
+    const int have = (int)min((int64_t)8, j.d - c * 8);
     if constexpr (sizeof(T) == 4) {
         float v[8];
-        load8(src + row * d + c * 8, have, v);
-        store_operand<T>((__bf16 *)dst + row * ld + c * 8, n * ld, v);
+        load8(src, have, v);
+        store_operand<T>((__bf16 *)j.dst + row * ld + c * 8, j.n * ld, v);
     } else {
         typedef T vec __attribute__((ext_vector_type(8)));
-        *reinterpret_cast<vec *>((T *)dst + row * ld + c * 8) = load8(src + row * d + c * 8, have);
+        *reinterpret_cast<vec *>((T *)j.dst + row * ld + c * 8) = load8(src, have);
     }
 }
 
@@ -122,11 +130,19 @@ hipError_t point(const GluPointArgs &a, hipStream_t st) {
 }
 
 template <typename T>
-hipError_t stage(const void *src, int64_t n, int64_t d, void *dst, hipStream_t st) {
-    const int64_t ld = dense_ld(d), blocks = (n * (ld / 8) + 255) / 256;
+hipError_t stage(const DenseStageJob *jobs, int count, hipStream_t st) {
+    StageJobs s{};
+    int64_t blocks = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (i < count) {
+            s.job[i] = jobs[i];
+            blocks += (jobs[i].n * (dense_ld(jobs[i].d) / 8) + 255) / 256;
+        }
+        s.blocks[i] = blocks;
+    }
     if (blocks > int64_t(1) << 34) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(dense_stage_kernel<T>, flat_grid(blocks, 256), dim3(256), 0, st, (const T *)src, n, d, ld,
-                       dst);
+    if (blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL(dense_stage_kernel<T>, flat_grid(blocks, 256), dim3(256), 0, st, s);
     return hipGetLastError();
 }
 
@@ -136,9 +152,8 @@ int64_t dense_ld(int64_t d) { return (d + 7) / 8 * 8; }
 int dense_planes(int prec) { return prec == P_FP32 ? 3 : 1; }
 bool dense_in_place(int prec, const void *p, int64_t d) { return prec != P_FP32 && d % 8 == 0 && (uintptr_t)p % 16 == 0; }
 
-hipError_t launch_dense_stage(int prec, const void *src, int64_t n, int64_t d, void *dst, hipStream_t st) {
-    if (prec == P_FP32) return stage<float>(src, n, d, dst, st);
-    return stage<uint16_t>(src, n, d, dst, st);
+hipError_t launch_dense_stage(int prec, const DenseStageJob *jobs, int count, hipStream_t st) {
+    return prec == P_FP32 ? stage<float>(jobs, count, st) : stage<uint16_t>(jobs, count, st);
 }
 
 // Enough workgroups for the chip, of 64 rows and more where there are many.
