@@ -325,7 +325,6 @@ __global__ __launch_bounds__(P::THREADS, 2) void dense_kernel(const DenseLaunch 
         issue_a(1, to);
         issued();
     };
-    auto next = [](int at) { return at == (P::BUFFERS - 1) * P::STAGE ? 0 : at + P::STAGE; };
     if constexpr (P::PHASED) {
         // A phase: reads for one quarter of the tile and copies for the stage that
         // comes into this buffer next, then the quarter's instructions.  The
@@ -350,8 +349,10 @@ __global__ __launch_bounds__(P::THREADS, 2) void dense_kernel(const DenseLaunch 
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         };
-        auto stage = [&](auto parity, int at) {
+        static_assert(P::BUFFERS == 2, "the buffer is a constant of each stage");
+        auto stage = [&](auto parity) {
             constexpr int own = 1 + decltype(parity)::value, others = 3 - own;
+            constexpr int at = decltype(parity)::value * P::STAGE, other_at = P::STAGE - at;
             read_a(0, at, av);
             issue_b(0, at);
             ready();
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(P::THREADS, 2) void dense_kernel(const DenseLaunch 
             issue_b(1, at);
             ready();
             quarter(1, 1, bv[0]);
-            read_b(0, next(at), bv[others]);
+            read_b(0, other_at, bv[others]);
             issue_a(1, at);
             issued();
             ready();
@@ -379,20 +380,16 @@ __global__ __launch_bounds__(P::THREADS, 2) void dense_kernel(const DenseLaunch 
         __builtin_amdgcn_s_barrier();
         if (wave >= 4) __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        int at = 0;
         for (int st = 0; st < stages; st += 2) {
-            stage(std::integral_constant<int, 0>(), at);
-            at = next(at);
-            if (st + 1 < stages) {
-                stage(std::integral_constant<int, 1>(), at);
-                at = next(at);
-            }
+            stage(std::integral_constant<int, 0>());
+            if (st + 1 < stages) stage(std::integral_constant<int, 1>());
         }
         if (wave < 4) __builtin_amdgcn_s_barrier();
     } else {
         // Two such workgroups share a CU, and each covers the other's waits.
 #pragma unroll
         for (int buf = 0; buf < P::BUFFERS - 1; ++buf) issue(buf * P::STAGE);
+        auto next = [](int at) { return at == (P::BUFFERS - 1) * P::STAGE ? 0 : at + P::STAGE; };
         int at = 0, to = (P::BUFFERS - 1) * P::STAGE;
         for (int st = 0; st < stages; ++st) {
             // (__syncthreads would wait for all copies)
