@@ -19,15 +19,39 @@ namespace exemcl {
 
 template <typename T, int GROUP>
 struct W4TilePlan {
-    static constexpr int WAVES = 8, THREADS = WAVES * 64, RT = 4, MT = 4, WN = 4;
-    static constexpr int PARTS = Operand<T>::PARTS, BUFFERS = PARTS == 1 ? 2 : 1;
-    static constexpr int GPB = kW4Block / GROUP, STEPS = GROUP / 32;
-    static constexpr int X = WAVES * 4 * PARTS * 1024;       // bytes of x in a stage
-    static constexpr int XS = GPB * WAVES * 16 * 4;          // its groups' sums
-    static constexpr int WORDS = WN * RT * GPB * 64;         // the weights' words
-    static constexpr int XS_AT = BUFFERS * X, WORDS_AT = XS_AT + 2 * XS, LDS = WORDS_AT + 2 * WORDS;
+    static constexpr int WAVES = 8, THREADS = WAVES * 64, RT = 4, WN = 4, WM = 2;
+    static constexpr int PARTS = Operand<T>::PARTS, MT = PARTS == 1 ? 4 : 2, XT = WM * MT, ROWS = XT * 16;
+    static constexpr int GPB = kW4Block / GROUP, STEPS = GROUP / 32;  // groups of a block, instructions of a group
+    static constexpr int UNITS = RT * GPB;                            // of a block: a tile, a group
+    static constexpr int SPW = XT * 4 / WAVES;                        // steps of x that a wavefront loads
+    static constexpr int SUMS = GPB > 4 / SPW ? GPB : 4 / SPW;        // partial sums of x in a block
+    static constexpr int X = XT * 4 * PARTS * 1024;                   // bytes of a block's x
+    static constexpr int XZ = XT * 1024, WZ = WN * RT * 1024;         // operands of the zero points' term
+    static constexpr int S = WN * RT * GPB * 64;                      // scales
+    static constexpr int XZ_AT = 2 * X, WZ_AT = XZ_AT + 2 * XZ, S_AT = WZ_AT + 2 * WZ, LDS = S_AT + 4 * S;
     static_assert(LDS <= kLdsBytes, "geometry");
 };
+
+// f(0), f(1), ... f(N - 1), the numbers as constants.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        each<N, I + 1>(f);
+    }
+}
+
+// The parts of a number in the places of the six products, and two zeros.
+template <bool FIRST>
+__device__ __forceinline__ bf16x8 six_places(float v, bool live) {
+    __bf16 part[3];
+    split_parts(live ? v : 0.0f, part[0], part[1], part[2]);
+    bf16x8 r;
+#pragma unroll
+    for (int p = 0; p < 6; ++p) r[p] = part[FIRST ? part_a(p) : part_b(p)];
+    r[6] = r[7] = (__bf16)0.0f;
+    return r;
+}
 
 template <typename T, int GROUP, bool GLU>
 __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
@@ -35,142 +59,201 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
     using E = typename Operand<T>::E;
     using vec = typename Mfma<E, 16>::vec_t;
     constexpr int RT = P::RT, MT = P::MT, GPB = P::GPB, STEPS = P::STEPS, PARTS = P::PARTS, MATS = GLU ? 2 : 1;
+    constexpr int UNITS = P::UNITS, SPW = P::SPW, SUMS = P::SUMS;
+    constexpr bool AHEAD = GROUP < 128;  // a second set of codes
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63, lr = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
 
     // Workgroups b, b + 8, ... share an XCD and its L2: blocks of rows that read the
     // same weights follow each other there.
-    const int64_t wg = flat_block(), pos = wg >> 3, unit = pos / a.mblocks * 8 + (wg & 7), mb = pos % a.mblocks;
+    const uint32_t wg = (uint32_t)flat_block(), pos = wg >> 3;
+    const int turn = __builtin_amdgcn_readfirstlane(pos / (uint32_t)a.mblocks), unit = turn * 8 + (int)(wg & 7);
     if (unit >= a.units) return;
-    const int64_t d = a.d, row0 = mb * 128, tile0 = unit * (P::WN * RT / MATS), ftiles = (a.f + 15) / 16;
-    const int blocks = (int)w4_blocks(d), whole = (int)(d / kW4Block);
+    const int d = (int)a.d, blocks = (int)w4_blocks(d), whole = d / kW4Block;
+    const int64_t row0 = (int64_t)((int)pos - turn * (int)a.mblocks) * P::ROWS;
+    const int tile0 = unit * (P::WN * RT / MATS), ftiles = (int)((a.f + 15) / 16);
 
-    const T *x = (const T *)a.x + min(row0 + wave * 16 + lr, a.n - 1) * d + 8 * g;
-    // Tile t of this wavefront (GLU: gate and up in turn), past the last one it again.
-    auto tile_of = [&](int wn, int t) { return min(tile0 + wn * (RT / MATS) + t / MATS, ftiles - 1); };
+    // Tile t of the workgroup's 16 (GLU: gate and up in turn), past the last one it
+    // again.
+    auto tile_of = [&](int t) { return (int64_t)min(tile0 + t / MATS, ftiles - 1); };
     const u32x4 *codes[RT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) codes[t] = (const u32x4 *)a.w[t % MATS] + tile_of(wn, t) * blocks * 64 + lane;
-    // Words: wavefront w < WN GPB / 4 copies 64 lanes' 16 bytes, 4 to a group of a tile.
-    constexpr int WORD_WAVES = P::WORDS / 1024;
-    const u32x4 *words;
-    {
-        const int q = (wave % WORD_WAVES) * 16 + (lane >> 2), t = q / GPB;
-        words = (const u32x4 *)a.words[t % RT % MATS] + (tile_of(t / RT, t % RT) * blocks * GPB + q % GPB) * 4 + (lane & 3);
+    for (int t = 0; t < RT; ++t) codes[t] = (const u32x4 *)a.w[t % MATS] + tile_of(wn * RT + t) * blocks * 64;
+    // This wavefront brings steps step0 .. of tile xt of x, in operand order, and the
+    // words of two tiles: lane (lr, g) the one of row lr for partial sum g.
+    const int xt = wave % P::XT, step0 = wave / P::XT * SPW, col0 = 32 * step0 + 8 * g;
+    const int64_t xrow = min(row0 + xt * 16, a.n - 1);
+    const T *x = (const T *)a.x + xrow * d;
+    const int xrow_at = (int)min((int64_t)lr, a.n - 1 - xrow) * d;
+    const int word_group = min(g, SUMS - 1) * GPB / SUMS, word_at = word_group * 16 + lr;
+    const uint32_t *words[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t = wave * 2 + i;
+        words[i] = (const uint32_t *)a.words[t % MATS] + tile_of(t) * blocks * GPB * 16;
     }
 
-    typename Chunk<T>::vec xr[4];
-    u32x4 cr[RT], c[RT], wr;
-    auto load = [&](int b) {
-        const int at = min(b, blocks - 1);  // past the last block it again, never used
+    typename Chunk<T>::vec xr[SPW];
+    uint32_t wr[2];
+    u32x4 c[RT], cr[AHEAD ? RT : 1];
+    // Past the last block it again, never used.
+    auto load_codes = [&](int t, int b) { return (codes[t] + (int64_t)min(b, blocks - 1) * 64)[lane]; };
+    auto load = [&](int b, auto full) {
+        const int at = min(b, blocks - 1);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) cr[t] = codes[t][at * 64];
-        if (wave < WORD_WAVES) wr = words[at * GPB * 4];
-        if (at < whole) {
+        for (int i = 0; i < 2; ++i) wr[i] = (words[i] + (int64_t)at * GPB * 16)[word_at];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) xr[j] = load8(x + at * kW4Block + 32 * j, 8);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = at * kW4Block + 32 * j;
-                xr[j] = load8(x + min((int64_t)k, d - 1 - 8 * g), (int)(d - 8 * g - k));
-            }
+        for (int j = 0; j < SPW; ++j) {
+            const int k = at * kW4Block + 32 * j + col0;
+            xr[j] = load8(x + (uint32_t)(xrow_at + (full ? k : min(k, d - 1))), full ? 8 : d - k);
         }
     };
-    // The loaded block into LDS.
+    // The loaded block into LDS: x, its sums as operands, the scales, and minus scale
+    // times zero point as operands.
     auto store = [&](int b) {
-        unsigned char *to = smem + b % P::BUFFERS * P::X;
+        unsigned char *to = smem + (b & 1) * P::X;
         vec ones;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ones[e] = (E)1.0f;
+        constexpr int HERE = SUMS * SPW / 4, EACH = SPW / HERE;  // sums of this wavefront, steps of each
+        float sum = 0.0f;
 #pragma unroll
-        for (int q = 0; q < GPB; ++q) {
-            f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int q = 0; q < HERE; ++q) {
+            f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-            for (int j = q * STEPS; j < (q + 1) * STEPS; ++j) {
+            for (int j = q * EACH; j < (q + 1) * EACH; ++j) {
                 const RowsFrag<T> f = rows_frag<T>(xr[j]);
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p)
-                    *reinterpret_cast<vec *>(to + ((wave * 4 + j) * PARTS + p) * 1024 + lane * 16) = f.part[p];
-                s = rows_mma_whole<T>(ones, f, s);
+                    *reinterpret_cast<vec *>(to + ((xt * 4 + step0 + j) * PARTS + p) * 1024 + lane * 16) = f.part[p];
+                s[j & 1] = rows_mma_whole<T>(ones, f, s[j & 1]);
             }
-            if (g == 0) reinterpret_cast<float *>(smem + P::XS_AT + (b & 1) * P::XS)[q * 128 + wave * 16 + lr] = s[0];
+            sum = g == wave / P::XT * HERE + q ? s[0][0] + s[1][0] : sum;
         }
-        if (wave < WORD_WAVES)
-            *reinterpret_cast<u32x4 *>(smem + P::WORDS_AT + (b & 1) * P::WORDS + wave * 1024 + lane * 16) = wr;
+        const int mine = wave / P::XT * HERE;
+        const bool own = g >= mine && g < mine + HERE, spare = g >= SUMS && wave < P::XT;
+        if (SPW == 4 || own || spare)  // (SPW 4: every lane)
+            *reinterpret_cast<bf16x8 *>(smem + P::XZ_AT + (b & 1) * P::XZ + xt * 1024 + lane * 16) = six_places<false>(sum, own);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int t = wave * 2 + i;
+            const float s = __uint_as_float(wr[i] & 0xffffff00u), z = (float)(wr[i] & 0xffu);
+            *reinterpret_cast<bf16x8 *>(smem + P::WZ_AT + (b & 1) * P::WZ + t * 1024 + lane * 16) = six_places<true>(-s * z, g < SUMS);
+            // (lanes past the sums have the last one's word)
+            reinterpret_cast<float *>(smem + P::S_AT + (b & 3) * P::S)[(t * GPB + word_group) * 16 + lr] = s;
+        }
     };
 
-    f32x4 acc[RT][MT];
+    f32x4 acc[RT][MT], p[MT], sc = {0.0f, 0.0f, 0.0f, 0.0f};
+    RowsFrag<T> xf[MT][STEPS];
+    vec wf[STEPS];
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
+    for (int m = 0; m < MT; ++m) {
+        p[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int m = 0; m < MT; ++m) acc[t][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    load(0);
-    store(0);
-#pragma unroll
-    for (int t = 0; t < RT; ++t) c[t] = cr[t];
-    __syncthreads();
-    for (int b = 0; b < blocks; ++b) {
-        load(b + 1);
-        const unsigned char *from = smem + b % P::BUFFERS * P::X + wm * MT * 4 * PARTS * 1024 + lane * 16;
-        const float *sums = reinterpret_cast<const float *>(smem + P::XS_AT + (b & 1) * P::XS) + wm * MT * 16 + lr;
-        const unsigned char *scales = smem + P::WORDS_AT + (b & 1) * P::WORDS + wn * RT * GPB * 64 + g * 16;
-#pragma unroll
-        for (int q = 0; q < GPB; ++q) {
-            RowsFrag<T> xf[PARTS == 1 ? MT : 1][STEPS];
-            float xs[MT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) xs[m] = sums[q * 128 + m * 16];
-            auto fragment = [&](int m, int j) {
-                RowsFrag<T> f;
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p)
-                    f.part[p] = *reinterpret_cast<const vec *>(from + ((m * 4 + q * STEPS + j) * PARTS + p) * 1024);
-                return f;
-            };
-            if constexpr (PARTS == 1)
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int j = 0; j < STEPS; ++j) xf[m][j] = fragment(m, j);
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                const u32x4 word = *reinterpret_cast<const u32x4 *>(scales + (t * GPB + q) * 64);
-                vec wf[STEPS];
-#pragma unroll
-                for (int j = 0; j < STEPS; ++j) wf[j] = w4_operand(c[t][q * STEPS + j], E());
-                f32x4 p[MT];
-#pragma unroll
-                for (int m = 0; m < MT; ++m) p[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int j = 0; j < STEPS; ++j)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m)
-                        p[m] = rows_mma_whole<T>(wf[j], PARTS == 1 ? xf[PARTS == 1 ? m : 0][j] : fragment(m, j), p[m]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float s = __uint_as_float(word[i] & 0xffffff00u), z = -(float)(word[i] & 0xffu);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[t][m][i] = fmaf(s, fmaf(z, xs[m], p[m][i]), acc[t][m][i]);
-                }
-                if (PARTS > 1 && t + 1 < RT) __builtin_amdgcn_sched_barrier(0);
-            }
-            // (left alone, the compiler puts these sums off to the stage's end, and
-            // keeps each group's products until then in memory)
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int m = 0; m < MT; ++m) asm volatile("" : "+v"(acc[t][m]));
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (P::BUFFERS == 1) __syncthreads();  // everyone has read this block
-        store(b + 1);
-#pragma unroll
-        for (int t = 0; t < RT; ++t) c[t] = cr[t];
-        __syncthreads();
+        for (int t = 0; t < RT; ++t) acc[t][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
+    auto read_x = [&](int b, int m, int step) {
+        RowsFrag<T> f;
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k)
+            f.part[k] = *reinterpret_cast<const vec *>(smem + (b & 1) * P::X + (((wm * MT + m) * 4 + step) * PARTS + k) * 1024 + lane * 16);
+        return f;
+    };
+    // The zero points' term of block b: for every partial sum of x the six products of
+    // its parts with those of - s z, one instruction for a tile and a block.
+    auto zeros = [&](int b) {
+        bf16x8 xz[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+            xz[m] = *reinterpret_cast<const bf16x8 *>(smem + P::XZ_AT + (b & 1) * P::XZ + (wm * MT + m) * 1024 + lane * 16);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const bf16x8 wz = *reinterpret_cast<const bf16x8 *>(smem + P::WZ_AT + (b & 1) * P::WZ + (wn * RT + t) * 1024 + lane * 16);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[t][m] = Mfma<__bf16, 16>::mma(wz, xz[m], 0, acc[t][m]);
+        }
+    };
+    // Unit u of block b: the instructions of tile u % RT for group u / RT, and between
+    // them the conversion of the next unit's weights, the sums of the unit before,
+    // and behind a group's last tile the next group's x.
+    auto work = [&](int b, auto number) {
+        constexpr int u = decltype(number)::value, t = u % RT, q = u / RT;
+        constexpr int nu = (u + 1) % UNITS, nt = nu % RT, nq = nu / RT, pt = (u + UNITS - 1) % UNITS % RT;
+        if constexpr (u != 2) __builtin_amdgcn_sched_barrier(0);  // (the next block's stores go between the second's instructions)
+        const f32x4 s_now = *reinterpret_cast<const f32x4 *>(smem + P::S_AT + (b & 3) * P::S + ((wn * RT + t) * GPB + q) * 64 + g * 16);
+        if constexpr (AHEAD && nq == 0) c[nt] = cr[nt];
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                if (j == 0) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[pt][m][i] = fmaf(sc[i], p[m][i], acc[pt][m][i]);
+                    p[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+                p[m] = rows_mma_whole<T>(wf[j], xf[m][j], p[m]);
+            }
+            if constexpr (t == RT - 1)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) xf[m][j] = read_x(u == UNITS - 1 ? b + 1 : b, m, (q + 1) % GPB * STEPS + j);
+            wf[j] = w4_operand(c[nt][nq * STEPS + j], E());
+        }
+        sc = s_now;
+        if constexpr (u == 0) zeros(b);
+        if constexpr (!AHEAD) c[nt] = load_codes(nt, nu == 0 ? b + 2 : b + 1);
+        if constexpr (AHEAD && u == RT - 1)
+#pragma unroll
+            for (int i = 0; i < RT; ++i) cr[i] = load_codes(i, b + 1);
+        // (left alone, the compiler puts the sums off to the block's end, and keeps
+        // the products until then in memory)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) asm volatile("" : "+v"(acc[pt][m]));
+    };
+    auto barrier = []() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        c[t] = load_codes(t, 0);
+        if constexpr (AHEAD) cr[t] = c[t];
+    }
+    load(0, std::false_type());
+    store(0);
+    load(1, std::false_type());
+    barrier();
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xf[m][j] = read_x(0, m, j);
+        wf[j] = w4_operand(c[0][j], E());
+    }
+    if constexpr (GPB == 1) c[0] = load_codes(0, 1);
+    // A block: in its second unit the next block goes to LDS, and is visible after the
+    // barrier before its last unit, which reads from it.
+    auto block = [&](int b, auto full) {
+        each<UNITS>([&](auto number) {
+            constexpr int u = decltype(number)::value;
+            if constexpr (u == UNITS - 1) barrier();
+            work(b, number);
+            if constexpr (u == 1) {
+                store(b + 1);
+                load(b + 2, full);
+            }
+        });
+    };
+    int b = 0;
+    for (; b + 2 < whole; ++b) block(b, std::true_type());
+    for (; b < blocks; ++b) block(b, std::false_type());
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[RT - 1][m][i] = fmaf(sc[i], p[m][i], acc[RT - 1][m][i]);
 
 #pragma unroll
     for (int t = 0; t < RT; t += MATS) {
@@ -213,7 +296,7 @@ hipError_t w4_tile_launch(RowsArgs a, hipStream_t st) {
         ready[dev].store(true, std::memory_order_release);
     }
     const int64_t tiles = P::WN * P::RT / (GLU ? 2 : 1);
-    a.mblocks = (a.n + 127) / 128;
+    a.mblocks = (a.n + P::ROWS - 1) / P::ROWS;
     a.units = ((a.f + 15) / 16 + tiles - 1) / tiles;
     const int64_t groups = (a.units + 7) / 8;
     if (groups > (int64_t(1) << 31) / a.mblocks) return hipErrorInvalidValue;
