@@ -26,9 +26,9 @@ struct W4TilePlan {
     static constexpr int SPW = XT * 4 / WAVES;                        // steps of x that a wavefront loads
     static constexpr int SUMS = GPB > 4 / SPW ? GPB : 4 / SPW;        // partial sums of x in a block
     static constexpr int X = XT * 4 * PARTS * 1024;                   // bytes of a block's x
-    static constexpr int XZ = XT * 1024, WZ = WN * RT * 1024;         // operands of the zero points' term
-    static constexpr int S = WN * RT * GPB * 64;                      // scales
-    static constexpr int XZ_AT = 2 * X, WZ_AT = XZ_AT + 2 * XZ, S_AT = WZ_AT + 2 * WZ, LDS = S_AT + 4 * S;
+    static constexpr int XS = SUMS * ROWS * 4;                        // its sums
+    static constexpr int S = WN * RT * GPB * 64;                      // scales; minus scales times zero points
+    static constexpr int XS_AT = 2 * X, S_AT = XS_AT + 4 * XS, SZ_AT = S_AT + 4 * S, LDS = SZ_AT + 4 * S;
     static_assert(LDS <= kLdsBytes, "geometry");
 };
 
@@ -39,18 +39,6 @@ __device__ __forceinline__ void each(F &&f) {
         f(std::integral_constant<int, I>());
         each<N, I + 1>(f);
     }
-}
-
-// The parts of a number in the places of the six products, and two zeros.
-template <bool FIRST>
-__device__ __forceinline__ bf16x8 six_places(float v, bool live) {
-    __bf16 part[3];
-    split_parts(live ? v : 0.0f, part[0], part[1], part[2]);
-    bf16x8 r;
-#pragma unroll
-    for (int p = 0; p < 6; ++p) r[p] = part[FIRST ? part_a(p) : part_b(p)];
-    r[6] = r[7] = (__bf16)0.0f;
-    return r;
 }
 
 template <typename T, int GROUP, bool GLU>
@@ -81,12 +69,13 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) codes[t] = (const u32x4 *)a.w[t % MATS] + tile_of(wn * RT + t) * blocks * 64;
     // This wavefront brings steps step0 .. of tile xt of x, in operand order, and the
-    // words of two tiles: lane (lr, g) the one of row lr for partial sum g.
+    // words of two tiles: lane (lr, g) those of row lr for group g (past the last one
+    // it again).
     const int xt = wave % P::XT, step0 = wave / P::XT * SPW, col0 = 32 * step0 + 8 * g;
     const int64_t xrow = min(row0 + xt * 16, a.n - 1);
     const T *x = (const T *)a.x + xrow * d;
     const int xrow_at = (int)min((int64_t)lr, a.n - 1 - xrow) * d;
-    const int word_group = min(g, SUMS - 1) * GPB / SUMS, word_at = word_group * 16 + lr;
+    const int word_at = min(g, GPB - 1) * 16 + lr;
     const uint32_t *words[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -109,15 +98,21 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
             xr[j] = load8(x + (uint32_t)(xrow_at + (full ? k : min(k, d - 1))), full ? 8 : d - k);
         }
     };
-    // The loaded block into LDS: x, its sums as operands, the scales, and minus scale
-    // times zero point as operands.
+    // The loaded block into LDS: x and its sums, the scales, and minus scale times
+    // zero point.
     auto store = [&](int b) {
         unsigned char *to = smem + (b & 1) * P::X;
         vec ones;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ones[e] = (E)1.0f;
         constexpr int HERE = SUMS * SPW / 4, EACH = SPW / HERE;  // sums of this wavefront, steps of each
-        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float s = __uint_as_float(wr[i] & 0xffffff00u), z = (float)(wr[i] & 0xffu);
+            const int at = (b & 3) * P::S + (wave * 2 + i) * GPB * 64 + word_at * 4;
+            *reinterpret_cast<float *>(smem + P::S_AT + at) = s;
+            *reinterpret_cast<float *>(smem + P::SZ_AT + at) = -s * z;
+        }
 #pragma unroll
         for (int q = 0; q < HERE; ++q) {
             f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
@@ -129,28 +124,19 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
                     *reinterpret_cast<vec *>(to + ((xt * 4 + step0 + j) * PARTS + p) * 1024 + lane * 16) = f.part[p];
                 s[j & 1] = rows_mma_whole<T>(ones, f, s[j & 1]);
             }
-            sum = g == wave / P::XT * HERE + q ? s[0][0] + s[1][0] : sum;
-        }
-        const int mine = wave / P::XT * HERE;
-        const bool own = g >= mine && g < mine + HERE, spare = g >= SUMS && wave < P::XT;
-        if (SPW == 4 || own || spare)  // (SPW 4: every lane)
-            *reinterpret_cast<bf16x8 *>(smem + P::XZ_AT + (b & 1) * P::XZ + xt * 1024 + lane * 16) = six_places<false>(sum, own);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int t = wave * 2 + i;
-            const float s = __uint_as_float(wr[i] & 0xffffff00u), z = (float)(wr[i] & 0xffu);
-            *reinterpret_cast<bf16x8 *>(smem + P::WZ_AT + (b & 1) * P::WZ + t * 1024 + lane * 16) = six_places<true>(-s * z, g < SUMS);
-            // (lanes past the sums have the last one's word)
-            reinterpret_cast<float *>(smem + P::S_AT + (b & 3) * P::S)[(t * GPB + word_group) * 16 + lr] = s;
+            // (the same in every lane group)
+            reinterpret_cast<float *>(smem + P::XS_AT + (b & 3) * P::XS)[(wave / P::XT * HERE + q) * P::ROWS + xt * 16 + lr] = s[0][0] + s[1][0];
         }
     };
 
-    f32x4 acc[RT][MT], p[MT], sc = {0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 acc[RT][MT], p[MT], sc = {0.0f, 0.0f, 0.0f, 0.0f}, sz = sc;
+    float xs[MT];
     RowsFrag<T> xf[MT][STEPS];
     vec wf[STEPS];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         p[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        xs[m] = 0.0f;
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[t][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -161,20 +147,6 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
             f.part[k] = *reinterpret_cast<const vec *>(smem + (b & 1) * P::X + (((wm * MT + m) * 4 + step) * PARTS + k) * 1024 + lane * 16);
         return f;
     };
-    // The zero points' term of block b: for every partial sum of x the six products of
-    // its parts with those of - s z, one instruction for a tile and a block.
-    auto zeros = [&](int b) {
-        bf16x8 xz[MT];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-            xz[m] = *reinterpret_cast<const bf16x8 *>(smem + P::XZ_AT + (b & 1) * P::XZ + (wm * MT + m) * 1024 + lane * 16);
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const bf16x8 wz = *reinterpret_cast<const bf16x8 *>(smem + P::WZ_AT + (b & 1) * P::WZ + (wn * RT + t) * 1024 + lane * 16);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) acc[t][m] = Mfma<__bf16, 16>::mma(wz, xz[m], 0, acc[t][m]);
-        }
-    };
     // Unit u of block b: the instructions of tile u % RT for group u / RT, and between
     // them the conversion of the next unit's weights, the sums of the unit before,
     // and behind a group's last tile the next group's x.
@@ -182,7 +154,17 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
         constexpr int u = decltype(number)::value, t = u % RT, q = u / RT;
         constexpr int nu = (u + 1) % UNITS, nt = nu % RT, nq = nu / RT, pt = (u + UNITS - 1) % UNITS % RT;
         if constexpr (u != 2) __builtin_amdgcn_sched_barrier(0);  // (the next block's stores go between the second's instructions)
-        const f32x4 s_now = *reinterpret_cast<const f32x4 *>(smem + P::S_AT + (b & 3) * P::S + ((wn * RT + t) * GPB + q) * 64 + g * 16);
+        const int s_at = (b & 3) * P::S + ((wn * RT + t) * GPB + q) * 64 + g * 16;
+        const f32x4 s_now = *reinterpret_cast<const f32x4 *>(smem + P::S_AT + s_at), z_now = *reinterpret_cast<const f32x4 *>(smem + P::SZ_AT + s_at);
+        float xs_now[MT];
+        if constexpr (t == 0)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const float *sums = reinterpret_cast<const float *>(smem + P::XS_AT + (b & 3) * P::XS) + (wm * MT + m) * 16 + lr;
+                xs_now[m] = sums[q * SUMS / GPB * P::ROWS];
+#pragma unroll
+                for (int i = 1; i < SUMS / GPB; ++i) xs_now[m] += sums[(q * SUMS / GPB + i) * P::ROWS];
+            }
         if constexpr (AHEAD && nq == 0) c[nt] = cr[nt];
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) {
@@ -190,7 +172,7 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
             for (int m = 0; m < MT; ++m) {
                 if (j == 0) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[pt][m][i] = fmaf(sc[i], p[m][i], acc[pt][m][i]);
+                    for (int i = 0; i < 4; ++i) acc[pt][m][i] = fmaf(sz[i], xs[m], fmaf(sc[i], p[m][i], acc[pt][m][i]));
                     p[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
                 }
                 p[m] = rows_mma_whole<T>(wf[j], xf[m][j], p[m]);
@@ -200,8 +182,10 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
                 for (int m = 0; m < MT; ++m) xf[m][j] = read_x(u == UNITS - 1 ? b + 1 : b, m, (q + 1) % GPB * STEPS + j);
             wf[j] = w4_operand(c[nt][nq * STEPS + j], E());
         }
-        sc = s_now;
-        if constexpr (u == 0) zeros(b);
+        sc = s_now, sz = z_now;
+        if constexpr (t == 0)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) xs[m] = xs_now[m];
         if constexpr (!AHEAD) c[nt] = load_codes(nt, nu == 0 ? b + 2 : b + 1);
         if constexpr (AHEAD && u == RT - 1)
 #pragma unroll
@@ -253,7 +237,7 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[RT - 1][m][i] = fmaf(sc[i], p[m][i], acc[RT - 1][m][i]);
+        for (int i = 0; i < 4; ++i) acc[RT - 1][m][i] = fmaf(sz[i], xs[m], fmaf(sc[i], p[m][i], acc[RT - 1][m][i]));
 
 #pragma unroll
     for (int t = 0; t < RT; t += MATS) {
