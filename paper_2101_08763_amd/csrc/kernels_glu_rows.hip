@@ -8,6 +8,7 @@ namespace {
 template <typename T>
 hipError_t run(const RowsArgs &r, hipStream_t st) {
     if (r.n <= 16) return rows_launch<T, 0, true, 1, 1, 1>(r, st);
+    if (r.n <= 32) return rows_launch<T, 0, true, 1, 2, 1>(r, st);
     return rows_launch<T, 0, true, 1, 4, 1>(r, st);
 }
 
