@@ -939,12 +939,12 @@ struct StagedRows {
     const void *ptr(const Pieces &t) const { return copied ? t.base + at : src; }
 };
 
-hipError_t stage_rows(int prec, const Pieces &t, std::initializer_list<const StagedRows *> rows, hipStream_t st) {
-    DenseStageJob jobs[3];
+// Those to lay out; returns their number.
+int stage_jobs(const Pieces &t, std::initializer_list<const StagedRows *> rows, DenseStageJob *jobs) {
     int count = 0;
     for (const StagedRows *r : rows)
         if (r->copied) jobs[count++] = {r->src, r->n, r->d, t.base + r->at};
-    return count ? launch_dense_stage(prec, jobs, count, st) : hipSuccess;
+    return count;
 }
 
 int run_glu(const GluArgs &a, int prec, hipStream_t st) {
@@ -957,7 +957,9 @@ int run_glu(const GluArgs &a, int prec, hipStream_t st) {
         if (rc) return rc;
         t.base = (char *)ws.ptr;
     }
-    if (stage_rows(prec, t, {&x, &wg, &wu}, st) != hipSuccess) return EXEMCL_EDEVICE;
+    DenseStageJob jobs[3];
+    const int count = stage_jobs(t, {&x, &wg, &wu}, jobs);
+    if (count && launch_dense_stage(prec, jobs, count, st) != hipSuccess) return EXEMCL_EDEVICE;
     const int64_t ld = dense_ld(a.d);
     // (the two weights' planes are equally far apart)
     const DenseArgs p{{x.ptr(t), nullptr, ld, a.n * ld}, {wg.ptr(t), wu.ptr(t), ld, a.f * ld}, a.n, a.f, a.d,
@@ -995,9 +997,9 @@ int run_glu_grad(const GluGradArgs &a, int prec, hipStream_t st) {
     if (rc) return rc;
     t.base = (char *)ws.ptr;
     float *partial = partial_bytes ? (float *)(t.base + partial_at) : nullptr;
-    if (stage_rows(prec, t, {&x, &wg, &wu}, st) != hipSuccess) return EXEMCL_EDEVICE;
     float *sum = db ? (float *)(t.base + sums) : nullptr;
-    const GluPointArgs p{a.dh, a.g, a.u, a.n, a.f, a.act, t.base + dg, t.base + du, parts, sum};
+    GluPointArgs p{a.dh, a.g, a.u, a.n, a.f, a.act, t.base + dg, t.base + du, parts, sum, {}, 0};
+    p.job_count = stage_jobs(t, {&x, &wg, &wu}, p.jobs);
     hipError_t e = launch_glu_point(prec, p, st);
     if (e == hipSuccess && a.dx) {
         const DenseArgs q{{t.base + dg, t.base + du, ldf, a.n * ldf}, {wg.ptr(t), wu.ptr(t), ldd, a.f * ldd},
@@ -1009,8 +1011,7 @@ int run_glu_grad(const GluGradArgs &a, int prec, hipStream_t st) {
                           a.f, a.d, a.n, nullptr, nullptr, 0, a.dwg, a.dwu, nullptr, nullptr, partial};
         e = launch_glu_dw(prec, q, st);
     }
-    if (e == hipSuccess && a.dbg) e = launch_column_sum(sum, parts, a.f, a.dbg, st);
-    if (e == hipSuccess && a.dbu) e = launch_column_sum(sum + parts * a.f, parts, a.f, a.dbu, st);
+    if (e == hipSuccess && db) e = launch_column_sum(sum, parts, a.f, a.dbg, 2, a.dbu, st);
     return status_of(e);
 }
 

@@ -360,6 +360,9 @@ struct GluPointArgs {
     void *dg, *du;
     int64_t parts;
     float *sums;
+    // Rows to lay out in the same launch.
+    DenseStageJob jobs[3];
+    int job_count;
 };
 int64_t glu_point_parts(int64_t n, int64_t f);
 hipError_t launch_glu_point(int prec, const GluPointArgs &a, hipStream_t st);
@@ -367,7 +370,8 @@ hipError_t launch_glu_point(int prec, const GluPointArgs &a, hipStream_t st);
 // `bytes` (an even number) zero bytes at p.
 hipError_t launch_zero_bytes(void *p, int64_t bytes, hipStream_t st);
 
-// out[c] = sum over g < G of partial[g * d + c], in 64 bits, in a fixed order.
-hipError_t launch_column_sum(const float *partial, int64_t G, int64_t d, float *out, hipStream_t st);
+// out[c] = sum over g < G of partial[g * d + c], in 64 bits, in a fixed order; with 2
+// arrays out2 the same of the G * d values behind (each nullable).
+hipError_t launch_column_sum(const float *partial, int64_t G, int64_t d, float *out, int arrays, float *out2, hipStream_t st);
 
 }  // namespace exemcl

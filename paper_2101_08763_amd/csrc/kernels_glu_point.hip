@@ -1,6 +1,7 @@
 // kernels_glu_point.hip -- the gated block's element-wise part of the gradient, and
 // rows laid out as operands of the tiled products.
 #include <algorithm>
+#include <type_traits>
 
 #include "glu_device.hpp"
 #include "mfma_kernels.hpp"
@@ -39,8 +40,7 @@ struct StageJobs {
     int64_t blocks[3];  // workgroups up to and with each
 };
 template <typename T>
-__global__ __launch_bounds__(256) void dense_stage_kernel(const StageJobs jobs) {
-    int64_t b = flat_block();
+__device__ __forceinline__ void stage_rows(const StageJobs &jobs, int64_t b) {
     const int which = b < jobs.blocks[0] ? 0 : b < jobs.blocks[1] ? 1 : 2;
     if (which) b -= jobs.blocks[which - 1];
     const DenseStageJob j = jobs.job[which];
@@ -57,6 +57,10 @@ __global__ __launch_bounds__(256) void dense_stage_kernel(const StageJobs jobs) 
         *reinterpret_cast<vec *>((T *)j.dst + row * ld + c * 8) = load8(src, have);
     }
 }
+template <typename T>
+__global__ __launch_bounds__(256) void dense_stage_kernel(const StageJobs jobs) {
+    stage_rows<T>(jobs, flat_block());
+}
 
 __global__ __launch_bounds__(256) void zero_bytes_kernel(uint16_t *__restrict__ p, int64_t count) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) p[i] = 0;
@@ -70,11 +74,15 @@ constexpr int kPointCols = 32, kPointRows = 8;
 template <typename T, int ACT>
 __global__ __launch_bounds__(kPointCols *kPointRows) void glu_point_kernel(
     const T *__restrict__ dh, const T *__restrict__ gate, const T *__restrict__ up, int64_t n, int64_t f, int64_t ld,
-    int64_t rows, typename Operand<T>::E *__restrict__ dg, typename Operand<T>::E *__restrict__ du,
-    float *__restrict__ sums) {
+    int64_t rows, uint32_t cblocks, int64_t parts, typename Operand<T>::E *__restrict__ dg,
+    typename Operand<T>::E *__restrict__ du, float *__restrict__ sums, const StageJobs jobs) {
+    using Raw = typename std::conditional<sizeof(T) == 4, float, uint16_t>::type;
+    const int64_t own = cblocks * parts, block = flat_block();
+    if (block >= own) return stage_rows<Raw>(jobs, block - own);
     __shared__ float part[kPointRows][kPointCols][17];
     const int cl = threadIdx.x % kPointCols, r = threadIdx.x / kPointCols;
-    const int64_t c = ((int64_t)blockIdx.x * kPointCols + cl) * 8, r0 = blockIdx.y * rows, r1 = min(n, r0 + rows);
+    const uint32_t p = (uint32_t)block / cblocks, cb = (uint32_t)block - p * cblocks;
+    const int64_t c = ((int64_t)cb * kPointCols + cl) * 8, r0 = p * rows, r1 = min(n, r0 + rows);
     const int have = (int)max((int64_t)0, min((int64_t)8, f - c));
     float sg[8] = {}, su[8] = {};
     if (c < ld)
@@ -105,8 +113,21 @@ __global__ __launch_bounds__(kPointCols *kPointRows) void glu_point_kernel(
         float s = 0.0f;
 #pragma unroll
         for (int q = 0; q < kPointRows; ++q) s += part[q][cl][r * 8 + i];
-        if (i < have) sums[((int64_t)r * gridDim.y + blockIdx.y) * f + c + i] = s;
+        if (i < have) sums[(r * parts + p) * f + c + i] = s;
     }
+}
+
+// The jobs' workgroups; returns their number.
+int64_t stage_jobs(const DenseStageJob *jobs, int count, StageJobs *s) {
+    int64_t blocks = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (i < count) {
+            s->job[i] = jobs[i];
+            blocks += (jobs[i].n * (dense_ld(jobs[i].d) / 8) + 255) / 256;
+        }
+        s->blocks[i] = blocks;
+    }
+    return blocks;
 }
 
 template <typename T>
@@ -114,9 +135,12 @@ hipError_t point(const GluPointArgs &a, hipStream_t st) {
     using E = typename Operand<T>::E;
     const int64_t ld = dense_ld(a.f), cb = (ld / 8 + kPointCols - 1) / kPointCols;
     const int64_t rows = (a.n + a.parts - 1) / a.parts;
+    StageJobs jobs{};
+    const int64_t blocks = cb * a.parts + stage_jobs(a.jobs, a.job_count, &jobs);
+    if (blocks > int64_t(1) << 34) return hipErrorInvalidValue;
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)cb, (unsigned)a.parts), dim3(kPointCols * kPointRows), 0, st,
-                           (const T *)a.dh, (const T *)a.g, (const T *)a.u, a.n, a.f, ld, rows, (E *)a.dg, (E *)a.du, a.sums);
+        hipLaunchKernelGGL(kern, flat_grid(blocks, 256), dim3(256), 0, st, (const T *)a.dh, (const T *)a.g, (const T *)a.u,
+                           a.n, a.f, ld, rows, (uint32_t)cb, a.parts, (E *)a.dg, (E *)a.du, a.sums, jobs);
     };
     if (a.act == ACT_SILU)
         go(glu_point_kernel<T, ACT_SILU>);
@@ -132,14 +156,7 @@ hipError_t point(const GluPointArgs &a, hipStream_t st) {
 template <typename T>
 hipError_t stage(const DenseStageJob *jobs, int count, hipStream_t st) {
     StageJobs s{};
-    int64_t blocks = 0;
-    for (int i = 0; i < 3; ++i) {
-        if (i < count) {
-            s.job[i] = jobs[i];
-            blocks += (jobs[i].n * (dense_ld(jobs[i].d) / 8) + 255) / 256;
-        }
-        s.blocks[i] = blocks;
-    }
+    const int64_t blocks = stage_jobs(jobs, count, &s);
     if (blocks > int64_t(1) << 34) return hipErrorInvalidValue;
     if (blocks == 0) return hipSuccess;
     hipLaunchKernelGGL(dense_stage_kernel<T>, flat_grid(blocks, 256), dim3(256), 0, st, s);

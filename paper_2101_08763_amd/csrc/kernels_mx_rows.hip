@@ -343,9 +343,11 @@ __global__ __launch_bounds__(256) void rmsnorm_dw_long_kernel(const T *__restric
 
 // dw[c] = sum over g of partial[g][c], in 64 bits and a fixed order.
 constexpr int kDwCols = 16, kDwRows = 64, kDwUnroll = 8;
+// (of a second array behind the first, too, where the grid has two rows)
 __global__ __launch_bounds__(kDwCols *kDwRows) void column_sum_kernel(const float *__restrict__ partial, int G, int d,
-                                                                       float *__restrict__ dw) {
+                                                                       float *__restrict__ dw, float *__restrict__ dw2) {
     __shared__ double part[kDwRows][kDwCols + 1];
+    partial += (int64_t)blockIdx.y * G * d;
     const int cl = threadIdx.x % kDwCols, q = threadIdx.x / kDwCols, c = blockIdx.x * kDwCols + cl;
     double s = 0.0;
     if (c < d)
@@ -363,7 +365,8 @@ __global__ __launch_bounds__(kDwCols *kDwRows) void column_sum_kernel(const floa
         if (q < w) part[q][cl] += part[q + w][cl];
         __syncthreads();
     }
-    if (q == 0 && c < d) dw[c] = (float)part[0][cl];
+    float *out = blockIdx.y ? dw2 : dw;
+    if (q == 0 && c < d && out) out[c] = (float)part[0][cl];
 }
 
 template <typename T, int BITS>
@@ -472,14 +475,14 @@ hipError_t grad_typed(const NormGradArgs &a, hipStream_t st) {
         }
     }
     if (e != hipSuccess || !a.dw) return e;
-    return launch_column_sum(a.partial, a.parts, a.d, a.dw, st);
+    return launch_column_sum(a.partial, a.parts, a.d, a.dw, 1, nullptr, st);
 }
 
 }  // namespace
 
-hipError_t launch_column_sum(const float *partial, int64_t G, int64_t d, float *out, hipStream_t st) {
-    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((d + kDwCols - 1) / kDwCols)), dim3(kDwCols * kDwRows), 0, st,
-                       partial, (int)G, (int)d, out);
+hipError_t launch_column_sum(const float *partial, int64_t G, int64_t d, float *out, int arrays, float *out2, hipStream_t st) {
+    hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((d + kDwCols - 1) / kDwCols), (unsigned)arrays),
+                       dim3(kDwCols * kDwRows), 0, st, partial, (int)G, (int)d, out, out2);
     return hipGetLastError();
 }
 
