@@ -428,7 +428,8 @@ EXEMCL_API int exemplar_mx_eval(const void *codes, const void *scales, int64_t n
  * may be NULL), and infinities and NaN go the way of arithmetic (of fp32 rows and
  * weights in exemplar_glu and its gradient an infinity may come out as NaN).  Outputs
  * must not overlap inputs.  All sums are in fp32 or wider, in an order that the
- * sizes decide: results are bitwise reproducible.
+ * sizes decide (and for the gradient the memory that is to be had): results are
+ * bitwise reproducible.
  *
  * Temporary memory, taken as exemplar_eval does: exemplar_glu_backward always (n > 0,
  * f > 0) and exemplar_glu of more than 64 rows where x, Wg or Wu has to be laid out
@@ -476,7 +477,9 @@ EXEMCL_API int exemplar_glu(const void *x, int64_t n, int64_t d, const void *Wg,
  * The products take dg and du rounded to the type (fp32: in three bf16 parts); the
  * sums dbg and dbu take them unrounded.  dx is one sum over both matrices.
  * Temporary memory: dg and du (4 n f bytes; fp32: 12 n f), up to 4096 f bytes for the
- * sums, and x, Wg and Wu where they have to be laid out again.
+ * sums, x, Wg and Wu where they have to be laid out again, and up to 1 GB of partial
+ * sums of products with few results and long sums (the call does without where that is
+ * not to be had).
  */
 EXEMCL_API int exemplar_glu_backward(const void *dh, const void *x, const void *Wg, const void *Wu, const void *g,
                                      const void *u, int64_t n, int64_t d, int64_t f, int precision, int activation,
@@ -496,7 +499,8 @@ EXEMCL_API int exemplar_glu_backward(const void *dh, const void *x, const void *
  *           16 i + r at (i dp/group + c) 16 + r.  A word is z (0 .. 255) in its last 8
  *           bits and an fp32 number in the others, s with 16 significant bits: any
  *           fp16 or bf16 number is one.
- * Rows past n have any codes and words; a group's coordinates past d any codes.
+ * Rows past n have any codes and words; coordinates past d any codes, and groups
+ * wholly past d words with a finite scale.
  */
 
 /*
@@ -527,7 +531,8 @@ EXEMCL_API int exemplar_w4_dequantize(const void *codes, const uint32_t *words, 
  * exemplar_w4_product -- y = x W' + bias for rows x (n x d, type per `precision`, not
  * rounded further) and weights of f rows of 4 bits; y is n x f of x's type, bias f
  * floats or NULL.  A group's products are added with whole q, and s and z applied to
- * the sum, in fp32.  No temporary memory.
+ * the sum, in fp32 (fp32 rows in three bf16 parts, all of each; an infinity in x may
+ * come out as NaN).  No temporary memory.
  */
 EXEMCL_API int exemplar_w4_product(const void *x, int64_t n, int64_t d, int precision, const void *codes,
                                    const uint32_t *words, int64_t f, int group, const float *bias, void *y, void *stream);

@@ -100,7 +100,7 @@ struct RowsArgs {
     const float *b[2];
     int act;
     void *y, *g, *u;
-    int64_t mblocks, units;
+    uint32_t mblocks, units;
 };
 
 // GROUP 0: weights of type T; else 4-bit ones with so many to a group.  RT tiles
@@ -118,9 +118,10 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
 
     // Workgroups b, b + 8, ... share an XCD: blocks of rows that read the same
     // weights follow each other there.
-    const int64_t wg = flat_block(), pos = wg >> 3, unit = pos / a.mblocks * 8 + (wg & 7), mb = pos % a.mblocks;
+    const uint32_t wg = (uint32_t)flat_block(), pos = wg >> 3;
+    const uint32_t turn = __builtin_amdgcn_readfirstlane(a.mblocks == 1 ? pos : pos / a.mblocks), unit = turn * 8 + (wg & 7);
     if (unit >= a.units) return;
-    const int64_t tile0 = unit * RT, row0 = mb * (16 * MT);
+    const int64_t tile0 = (int64_t)unit * RT, row0 = (int64_t)(pos - turn * a.mblocks) * (16 * MT);
     const int64_t d = a.d, ftiles = (a.f + 15) / 16;
 
     const T *x[MT];
@@ -290,13 +291,21 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
     }
 }
 
+// Blocks of `rows` rows by units of `weights` weights' rows, 8 units at a time over
+// the XCDs.
+inline hipError_t rows_grid(RowsArgs &a, int64_t rows, int64_t weights) {
+    const int64_t mblocks = (a.n + rows - 1) / rows, units = (a.f + weights - 1) / weights;
+    if ((units + 7) / 8 > (int64_t(1) << 28) / mblocks) return hipErrorInvalidValue;  // 32 bits of workgroups
+    a.mblocks = (uint32_t)mblocks, a.units = (uint32_t)units;
+    return hipSuccess;
+}
+inline int64_t rows_workgroups(const RowsArgs &a) { return (int64_t)((a.units + 7) / 8) * 8 * a.mblocks; }
+
 template <typename T, int GROUP, bool GLU, int RT, int MT, int AHEAD>
 hipError_t rows_launch(RowsArgs a, hipStream_t st) {
-    a.mblocks = (a.n + 16 * MT - 1) / (16 * MT);
-    a.units = ((a.f + 15) / 16 + RT - 1) / RT;
-    const int64_t groups = (a.units + 7) / 8;
-    if (groups > (int64_t(1) << 31) / a.mblocks) return hipErrorInvalidValue;  // 2^14 rows of kFlatRow
-    hipLaunchKernelGGL((rows_kernel<T, GROUP, GLU, RT, MT, AHEAD>), flat_grid(groups * 8 * a.mblocks, kRowsWaves * 64),
+    const hipError_t e = rows_grid(a, 16 * MT, 16 * RT);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((rows_kernel<T, GROUP, GLU, RT, MT, AHEAD>), flat_grid(rows_workgroups(a), kRowsWaves * 64),
                        dim3(kRowsWaves * 64), 0, st, a);
     return hipGetLastError();
 }

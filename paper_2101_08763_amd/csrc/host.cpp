@@ -991,12 +991,17 @@ int run_glu_grad(const GluGradArgs &a, int prec, hipStream_t st) {
     // (one after the other on the stream: they share their partial sums' memory)
     const int64_t partial_bytes = std::max(a.dx ? glu_dx_partial(prec, a.n, a.d, a.f) : 0,
                                            dw ? glu_dw_partial(prec, a.f, a.d, a.n, a.dwg && a.dwu ? 2 : 1) : 0);
-    const int64_t partial_at = t.take(partial_bytes);
+    const int64_t partial_at = t.bytes;
     Scratch ws;
-    const int rc = alloc_uncaptured(&ws, t.bytes, workspace_limit(), st);
+    bool split = partial_bytes > 0;
+    int rc = alloc_uncaptured(&ws, t.bytes + partial_bytes, workspace_limit(), st);
+    if (rc == EXEMCL_ENOMEM && split) {
+        split = false;
+        rc = alloc_uncaptured(&ws, t.bytes, workspace_limit(), st);
+    }
     if (rc) return rc;
     t.base = (char *)ws.ptr;
-    float *partial = partial_bytes ? (float *)(t.base + partial_at) : nullptr;
+    float *partial = split ? (float *)(t.base + partial_at) : nullptr;
     float *sum = db ? (float *)(t.base + sums) : nullptr;
     GluPointArgs p{a.dh, a.g, a.u, a.n, a.f, a.act, t.base + dg, t.base + du, parts, sum, {}, 0};
     p.job_count = stage_jobs(t, {&x, &wg, &wu}, p.jobs);

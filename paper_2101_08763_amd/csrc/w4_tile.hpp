@@ -56,8 +56,8 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
     // Workgroups b, b + 8, ... share an XCD and its L2: blocks of rows that read the
     // same weights follow each other there.
     const uint32_t wg = (uint32_t)flat_block(), pos = wg >> 3;
-    const int turn = __builtin_amdgcn_readfirstlane(pos / (uint32_t)a.mblocks), unit = turn * 8 + (int)(wg & 7);
-    if (unit >= a.units) return;
+    const int turn = __builtin_amdgcn_readfirstlane(pos / a.mblocks), unit = turn * 8 + (int)(wg & 7);
+    if ((uint32_t)unit >= a.units) return;
     const int d = (int)a.d, blocks = (int)w4_blocks(d), whole = d / kW4Block;
     const int64_t row0 = (int64_t)((int)pos - turn * (int)a.mblocks) * P::ROWS;
     const int tile0 = unit * (P::WN * RT / MATS), ftiles = (int)((a.f + 15) / 16);
@@ -279,12 +279,9 @@ hipError_t w4_tile_launch(RowsArgs a, hipStream_t st) {
         if (e != hipSuccess) return e;
         ready[dev].store(true, std::memory_order_release);
     }
-    const int64_t tiles = P::WN * P::RT / (GLU ? 2 : 1);
-    a.mblocks = (a.n + P::ROWS - 1) / P::ROWS;
-    a.units = ((a.f + 15) / 16 + tiles - 1) / tiles;
-    const int64_t groups = (a.units + 7) / 8;
-    if (groups > (int64_t(1) << 31) / a.mblocks) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(kern, flat_grid(groups * 8 * a.mblocks, P::THREADS), dim3(P::THREADS), P::LDS, st, a);
+    const hipError_t e = rows_grid(a, P::ROWS, 16 * P::WN * P::RT / (GLU ? 2 : 1));
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, flat_grid(rows_workgroups(a), P::THREADS), dim3(P::THREADS), P::LDS, st, a);
     return hipGetLastError();
 }
 

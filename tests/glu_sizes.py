@@ -13,3 +13,6 @@ LARGE = [(4100, 40, 2060), (4100, 2090, 130), (130, 1300, 2900)]
 # Products by 4-bit weights (n, d, f).
 W4 = [(1, 1, 1), (1, 40, 300), (1, 1301, 77), (3, 129, 33), (7, 2000, 15), (16, 128, 130), (17, 64, 257), (33, 7, 19),
       (64, 520, 100), (65, 384, 100), (200, 301, 70), (300, 1000, 530)]
+# Enough rows for tiles through LDS: several blocks of 128 coordinates and one of less,
+# one block, one coordinate.
+W4_LARGE = [(2900, 700, 1500), (2500, 520, 150), (3000, 100, 700), (6000, 1, 40)]

@@ -222,6 +222,26 @@ def test_activations_far_out(act, t):
 half = ref.half
 
 
+@pytest.mark.parametrize("n", [3, 100])
+def test_subnormal_fp16(n):
+    """Numbers below 2^-14 count with all their bits: weights of k 2^-24 times rows of
+    1024 (sums of k, exactly), and rows of k 2^-24 times weights of 1024."""
+    d, f, t = 64, 48, torch.float16
+    r = gen("subnormal", n)
+    k = torch.randint(-500, 500, (f, d), generator=r, device="cuda")
+    W = (k.double() * 2.0 ** -24).to(t)
+    x = torch.full((n, d), 1024.0, dtype=t, device="cuda")
+    _, g, u = api.exemplar_glu(x, W, W, save=True)
+    want = (k.sum(1).double() * 2.0 ** -14)[None].expand(n, f)
+    assert torch.equal(g.double(), want.to(t).double()) and torch.equal(u, g)
+    kx = torch.randint(-500, 500, (n, d), generator=r, device="cuda")
+    q = api.exemplar_w4_quantize(torch.full((f, d), 1024.0, device="cuda"), 32)
+    values = api.exemplar_w4_dequantize(q, torch.float32).double()
+    y = api.exemplar_w4_product((kx.double() * 2.0 ** -24).to(t), q)
+    want = ref.times(kx.double() * 2.0 ** -24, values)
+    close(y, want, 2.0 ** -11 * want.abs() + 2.0 ** -24)
+
+
 def test_empty():
     x, W = torch.ones(0, 8, device="cuda"), torch.ones(6, 8, device="cuda")
     h, g, u = api.exemplar_glu(x, W, W, save=True)
@@ -335,7 +355,28 @@ def test_w4_glu(at, size, t, group):
     assert untouched(flat, at % 2)
 
 
-@pytest.mark.parametrize("n", [1, 70])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("t", TYPES, ids=str)
+@pytest.mark.parametrize("size", glu_sizes.W4_LARGE, ids=str)
+def test_w4_on_many_rows(size, t, group):
+    n, d, f = size
+    g = gen("w4 many", size, str(t), group)
+    (qg, Wg), (qu, Wu) = weights(g, f, d, group), weights(g, f, d, group)
+    x, bias = randn(g, n, d).to(t), randn(g, f)
+    flat, out = inside((n, f), t, 1)
+    api.exemplar_w4_product(among_nan(x), qg, bias=bias, out=out)
+    y, _, bound = w4_bounds(x.double(), Wg, qg, bias.double(), t)
+    close(out, y, bound)
+    assert untouched(flat, 1) and torch.equal(api.exemplar_w4_product(x, qg, bias=bias), out)
+    h = api.exemplar_w4_glu(x, qg, qu, bias, None)
+    G, eg, _ = w4_bounds(x.double(), Wg, qg, bias.double(), t)
+    U, eu, _ = w4_bounds(x.double(), Wu, qu, None, t)
+    a, _ = ref.activation("silu", G)
+    e = 1.2 * eg * (U.abs() + eu) + (a.abs() + ref.act_bound(t) * G.abs()) * eu + ref.act_bound(t) * G.abs() * U.abs()
+    close(h, a * U, e + ref.half(t) * ((a * U).abs() + e) + ref.TINY[t])
+
+
+@pytest.mark.parametrize("n", [1, 70, 2000])
 def test_w4_words_of_any_kind(n):
     """Zero points up to 255, scales of either sign, codes and words of rows past n
     of any kind, and NaN scales."""
@@ -397,6 +438,104 @@ def test_captured_and_replayed():
         api.exemplar_glu_backward(want[0], x, Wg, Wu, want[1], want[2])
 
 
+# -- streams -------------------------------------------------------------------------
+def _on_streams():
+    import test_streams_gpu as streams
+    return streams
+
+
+@pytest.fixture(scope="module")
+def made():
+    r = gen("streams")
+    n, d, f = 1500, 256, 1000
+    x, Wg, Wu, bg, bu = block(r, n, d, f, torch.bfloat16, True)
+    q = api.exemplar_w4_quantize(Wg, 64)
+    return x, Wg, Wu, bg, bu, randn(r, n, f).bfloat16(), q
+
+
+CALLS = {
+    "glu": (lambda m: m[:5], lambda a, st: api.exemplar_glu(*a, save=True, stream=st)),
+    "glu_fp32": (lambda m: tuple(t.float() for t in m[:3]), lambda a, st: api.exemplar_glu(*a, stream=st)[:1]),
+    "glu_backward": (lambda m: (m[5], m[0], m[1], m[2], m[5].clone(), m[5].clone()),
+                     lambda a, st: api.exemplar_glu_backward(*a, bias=True, stream=st)),
+    "w4_quantize": (lambda m: (m[1],), lambda a, st: api.exemplar_w4_quantize(a[0], 32, stream=st)),
+    "w4_dequantize": (lambda m: (m[6],), lambda a, st: api.exemplar_w4_dequantize(a[0], torch.float32, stream=st)),
+    "w4_product": (lambda m: (m[0], m[6], m[3]), lambda a, st: api.exemplar_w4_product(*a, stream=st)),
+    "w4_glu": (lambda m: (m[0], m[6], m[6], m[3], m[4]), lambda a, st: api.exemplar_w4_glu(*a, stream=st)),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_memory_of_a_call_on_another_stream(name, made, monkeypatch):
+    """As the other calls do it: whose memory results are, and when memory that is
+    freed early is used again."""
+    streams = _on_streams()
+    monkeypatch.setattr(streams, "CALLS", CALLS)
+
+    def copies(a):
+        return tuple(x._replace(codes=x.codes.clone(), words=x.words.clone()) if isinstance(x, api.W4Rows) else x.clone()
+                     for x in a)
+
+    monkeypatch.setattr(streams, "copies", copies)
+    streams.test_memory_of_a_call_on_another_stream(name, made)
+
+
+def test_calls_from_several_threads():
+    """Threads that share a stream, and threads with streams of their own, get the
+    results of calls made one after the other."""
+    import threading
+    r = gen("threads")
+    n, d, f, t = 200, 136, 150, torch.float32
+    sets = [block(gen("threads", i), n, d, f, t, False)[:3] for i in range(4)]
+    dh = randn(r, n, f)
+    want = []
+    for x, Wg, Wu in sets:
+        h, g, u = api.exemplar_glu(x, Wg, Wu, save=True)
+        want.append([h, *api.exemplar_glu_backward(dh, x, Wg, Wu, g, u)[:3]])
+    torch.cuda.synchronize()
+    got = [None] * 8
+
+    def work(i):
+        x, Wg, Wu = sets[i % 4]
+        st = torch.cuda.Stream() if i >= 4 else None
+        with torch.cuda.stream(st or torch.cuda.current_stream()):
+            for _ in range(5):
+                h, g, u = api.exemplar_glu(x, Wg, Wu, save=True)
+                out = [h, *api.exemplar_glu_backward(dh, x, Wg, Wu, g, u)[:3]]
+        torch.cuda.synchronize()
+        got[i] = out
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(8)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    for i in range(8):
+        assert all(torch.equal(a, b) for a, b in zip(got[i], want[i % 4])), i
+
+
+def test_gradient_within_a_workspace_limit(monkeypatch):
+    """Without memory for partial sums the products are not divided; without memory
+    for the rest the call is refused."""
+    n, d, f, t = 4000, 64, 72, torch.bfloat16
+    r = gen("limit")
+    x, Wg, Wu, _, _ = block(r, n, d, f, t, False)
+    dh, g, u = (randn(r, n, f).to(t) for _ in range(3))
+    args = (dh, x, Wg, Wu, g, u)
+    want, bounds = ref.glu_backward(*wide(*args), "silu"), ref.backward_bounds(*wide(*args), "silu", t)
+    own = 2 * n * f * 2
+    for limit in (None, own + 4096, own - 4096):
+        if limit:
+            monkeypatch.setenv("EXEMCL_WORKSPACE_LIMIT", str(limit))
+        if limit and limit < own:
+            with pytest.raises(api.ExemclError) as e:
+                api.exemplar_glu_backward(*args)
+            assert e.value.status == api.EXEMCL_ENOMEM
+            continue
+        for a, w, b in zip(api.exemplar_glu_backward(*args)[:3], want, bounds):
+            close(a, w, b)
+
+
 # -- together -----------------------------------------------------------------------
 def test_norm_block_and_products_together():
     """A residual block as it is trained and served: norm, gated block, the product
@@ -429,3 +568,39 @@ def test_norm_block_and_products_together():
         # 4-bit weights: a step of a sixteenth of the range is 1/3 of a weight's
         # size, half of it at most, 1/10 on average, and so for both factors of h
         assert float((s.double() - act[:rows].double()).square().mean() / act[:rows].double().square().mean()) < 0.15 ** 2 * 2
+
+
+def example():
+    spec = importlib.util.spec_from_file_location(
+        "gated_block", pathlib.Path(__file__).parent.parent / "examples" / "gated_block.py")
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+def test_example_runs():
+    losses, off, f = example().main(["--n", "700", "--width", "192", "--inner", "320", "--steps", "3"])
+    assert len(losses) == 3 and all(np.isfinite(losses)) and np.isfinite(off) and bool(f.isfinite().all())
+
+
+def test_example_gradients():
+    """The example's gradients against PyTorch's of the whole block in 64 bits.  Off by
+    roundings to bf16 (half a step 2^-9): of y, of g and u, of dh, of dg, of the result,
+    of h in no gradient; each moves a term of the sums by chance, so the root mean
+    square of all is within sqrt(5) 2^-9 and a factor of 2 for slopes above 1."""
+    ex, (n, d, f) = example(), (300, 96, 160)
+    r = gen("example")
+    x = randn(r, n, d).bfloat16()
+    Wg, Wu = ((randn(r, f, d) / d ** 0.5).bfloat16() for _ in range(2))
+    Wd = (randn(r, d, f) / f ** 0.5).bfloat16()
+    dz = randn(r, n, d)
+    _, kept = ex.forward(x, Wg, Wu, Wd)
+    got = ex.gradients(dz, kept, Wg, Wu, Wd)
+    leaves = [Wg.double().requires_grad_(), Wu.double().requires_grad_()]
+    x64 = x.double()
+    y = x64 / torch.sqrt((x64 * x64).mean(1, keepdim=True) + ex.EPS)
+    z = x64 + (torch.nn.functional.silu(y @ leaves[0].t()) * (y @ leaves[1].t())) @ Wd.double().t()
+    z.backward(dz.double())
+    for a, w in zip(got, leaves):
+        off = float((a.double() - w.grad).square().mean().sqrt() / w.grad.square().mean().sqrt())
+        assert off < 2 * 5 ** 0.5 * 2.0 ** -9, off
