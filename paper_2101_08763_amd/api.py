@@ -434,7 +434,7 @@ def _run(name, tensors, stream, *args):
     microseconds each, so the common case takes the short way."""
     dev = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (dev < 0 or t.get_device() != dev or not t.is_contiguous() or t.requires_grad):
+        if t is not None and (t.get_device() != dev or not t.is_contiguous() or t.requires_grad or dev < 0):
             _check_gradient(name, tensors)
             _check_device(*tensors)
     fn = getattr(_LIB or load(), name)
@@ -618,11 +618,11 @@ def _w4_check(q, name):
     codes, words, n, d, group = q
     if group != 128 and group != 64 and group != 32:
         raise ValueError(f"{name}: groups have 32, 64 or 128 coordinates")
-    if n < 0 or not 1 <= d <= 1 << 22:
+    if n < 0 or not 1 <= d <= 4194304:
         raise ValueError(f"{name}: rows have 1 to 2^22 coordinates, and there are not less than 0")
-    tiles, blocks = (n + 15) // 16, (d + 127) // 128
+    tiles, blocks = n + 15 >> 4, d + 127 >> 7
     uint8, int32 = _W4_TYPES or _w4_types()
-    if codes.dtype != uint8 or words.dtype != int32 or codes.shape != (tiles, blocks, 1024) \
+    if codes.dtype is not uint8 or words.dtype is not int32 or codes.shape != (tiles, blocks, 1024) \
             or words.shape != (tiles, blocks * 128 // group, 16):
         raise ValueError(f"{name}: codes must be uint8 {tiles} x {blocks} x 1024 and words int32 "
                          f"{tiles} x {blocks * 128 // group} x 16")
@@ -668,16 +668,20 @@ def exemplar_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, save=False
     prec = _precision(dtype)
     n, d = x.shape
     f = Wg.shape[0]
-    if Wg.dtype != dtype or Wu.dtype != dtype or Wg.shape[1] != d or Wu.shape != Wg.shape:
+    if Wg.dtype is not dtype or Wu.dtype is not dtype or Wg.shape != (f, d) or Wu.shape != (f, d):
         raise ValueError("Wg and Wu must have x's type, one shape and x's number of columns")
-    _bias_check(bg, f, "bg")
-    _bias_check(bu, f, "bu")
+    if bg is not None:
+        _bias_check(bg, f, "bg")
+    if bu is not None:
+        _bias_check(bu, f, "bu")
     h = _out(out, (n, f), x, stream)
     g = u = None
     if save:
         g, u = _out(None, (n, f), x, stream), _out(None, (n, f), x, stream)
-    _run("exemplar_glu", (x, Wg, Wu, bg, bu, h), stream, x.data_ptr(), n, d, Wg.data_ptr(), Wu.data_ptr(), f, _at(bg),
-         _at(bu), prec, activation, h.data_ptr(), _at(g), _at(u))
+    _run("exemplar_glu", (x, Wg, Wu) if bg is None and bu is None and out is None else (x, Wg, Wu, bg, bu, out), stream,
+         x.data_ptr(), n, d, Wg.data_ptr(), Wu.data_ptr(), f, None if bg is None else bg.data_ptr(),
+         None if bu is None else bu.data_ptr(), prec, activation, h.data_ptr(), None if g is None else g.data_ptr(),
+         None if u is None else u.data_ptr())
     return h, g, u
 
 
@@ -754,17 +758,21 @@ def exemplar_w4_product(x, W, bias=None, out=None, stream=None):
     if x.dim() != 2:
         raise ValueError("x must be n x d")
     dtype = x.dtype
-    prec = _precision(dtype)
+    prec = _PRECISIONS.get(dtype)
+    if prec is None:
+        prec = _precision(dtype)
     n, d = x.shape
     _w4_check(W, "W")
     codes, words, f, wd, group = W
     if wd != d:
         raise ValueError("x and W must have the same number of coordinates")
-    _bias_check(bias, f, "bias")
-    out = _out(out, (n, f), x, stream)
-    _run("exemplar_w4_product", (x, codes, words, bias, out), stream, x.data_ptr(), n, d, prec, codes.data_ptr(),
-         words.data_ptr(), f, group, _at(bias), out.data_ptr())
-    return out
+    if bias is not None:
+        _bias_check(bias, f, "bias")
+    y = _out(out, (n, f), x, stream)
+    _run("exemplar_w4_product", (x, codes, words) if bias is None and out is None else (x, codes, words, bias, out), stream,
+         x.data_ptr(), n, d, prec, codes.data_ptr(), words.data_ptr(), f, group, None if bias is None else bias.data_ptr(),
+         y.data_ptr())
+    return y
 
 
 def exemplar_w4_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, out=None, stream=None):
@@ -773,20 +781,26 @@ def exemplar_w4_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, out=Non
     if x.dim() != 2:
         raise ValueError("x must be n x d")
     dtype = x.dtype
-    prec = _precision(dtype)
+    prec = _PRECISIONS.get(dtype)
+    if prec is None:
+        prec = _precision(dtype)
     n, d = x.shape
     _w4_check(Wg, "Wg")
     _w4_check(Wu, "Wu")
-    f = Wg.n
-    if Wg.d != d or Wu.d != d or Wu.n != f or Wu.group != Wg.group:
+    gc, gw, f, gd, group = Wg
+    uc, uw, uf, ud, ugroup = Wu
+    if gd != d or ud != d or uf != f or ugroup != group:
         raise ValueError("Wg and Wu must have x's number of coordinates, one number of rows and one group size")
-    _bias_check(bg, f, "bg")
-    _bias_check(bu, f, "bu")
-    out = _out(out, (n, f), x, stream)
-    _run("exemplar_w4_glu", (x, Wg.codes, Wg.words, Wu.codes, Wu.words, bg, bu, out), stream, x.data_ptr(), n, d, prec,
-         Wg.codes.data_ptr(), Wg.words.data_ptr(), Wu.codes.data_ptr(), Wu.words.data_ptr(), f, Wg.group, _at(bg), _at(bu),
-         activation, out.data_ptr())
-    return out
+    if bg is not None:
+        _bias_check(bg, f, "bg")
+    if bu is not None:
+        _bias_check(bu, f, "bu")
+    h = _out(out, (n, f), x, stream)
+    few = bg is None and bu is None and out is None
+    _run("exemplar_w4_glu", (x, gc, gw, uc, uw) if few else (x, gc, gw, uc, uw, bg, bu, out), stream, x.data_ptr(), n, d, prec,
+         gc.data_ptr(), gw.data_ptr(), uc.data_ptr(), uw.data_ptr(), f, group, None if bg is None else bg.data_ptr(),
+         None if bu is None else bu.data_ptr(), activation, h.data_ptr())
+    return h
 
 
 def exemplar_plan(n: int, d: int, l: int, k: int, precision: int = EXEMCL_FP32):
