@@ -432,10 +432,10 @@ EXEMCL_API int exemplar_mx_eval(const void *codes, const void *scales, int64_t n
  * bitwise reproducible.
  *
  * Temporary memory, taken as exemplar_eval does: exemplar_glu_backward always (n > 0,
- * f > 0) and exemplar_glu of more than 64 rows where x, Wg or Wu has to be laid out
- * again (fp32, d not a multiple of 8, an address not a multiple of 16 bytes).  On a
- * capturing stream those calls return EINVAL and queue nothing; the others may be
- * captured.
+ * f > 0) and exemplar_glu, of more than 64 rows, where x, Wg or Wu has to be laid out
+ * again (fp32, d not a multiple of 8, an address not a multiple of 16 bytes) and the
+ * sizes are better served that way.  On a capturing stream those calls return EINVAL
+ * and queue nothing; the others may be captured.
  * ------------------------------------------------------------------------ */
 enum exemcl_activation {
     EXEMCL_SILU = 0,      /* g / (1 + e^-g) */

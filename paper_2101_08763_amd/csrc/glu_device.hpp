@@ -76,18 +76,31 @@ __device__ __forceinline__ void with_activation(int act, F &&f) {
 // three bf16 ones (hi + mid + lo, each the rounding of what is left), and a
 // product of two the six products of parts that are not below 2^-27 of it, added
 // in the fp32 accumulators: 2.7 times the fp32 instruction's rate.  A value that
-// rounds to an infinity keeps its upper bits instead, and an infinity or NaN
-// has no other parts.
+// would round to an infinity keeps the largest bf16 as its upper part.  Of an
+// infinity that leaves one, whose rest is NaN; a NaN is NaN from the second part on.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ void split_parts(float x, __bf16 &hi, __bf16 &mid, __bf16 &lo) {
-    const uint32_t bits = __float_as_uint(x);
-    __bf16 h = (__bf16)x;
-    if ((bits & 0x7fffffffu) >= 0x7f7f8000u)  // past the largest bf16
-        h = __builtin_bit_cast(__bf16, (uint16_t)((bits >> 16) | ((bits & 0x7fffffffu) > 0x7f800000u ? 0x40u : 0u)));
-    const float r = (bits & 0x7f800000u) == 0x7f800000u ? 0.0f : x - (float)h;
-    hi = h;
-    mid = (__bf16)r;
-    lo = (__bf16)(r - (float)mid);
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ void split_parts(f32x8 x, bf16x8 &hi, bf16x8 &mid, bf16x8 &lo) {
+    typedef float pair __attribute__((ext_vector_type(2)));
+    typedef __bf16 rounded __attribute__((ext_vector_type(2)));
+    constexpr float kMost = 0x1.fefffep+127f;  // rounds to the largest bf16
+    uint32_t part[3][4];
+    // A dword of two rounded values, and the values without them: one conversion for both.
+    auto take = [](pair &v, pair from) {
+        const uint32_t bits = __builtin_bit_cast(uint32_t, __builtin_convertvector(from, rounded));
+        v -= pair{__uint_as_float(bits << 16), __uint_as_float(bits & 0xffff0000u)};
+        return bits;
+    };
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        pair v{x[2 * e], x[2 * e + 1]};
+        part[0][e] = take(v, pair{__builtin_amdgcn_fmed3f(v[0], -kMost, kMost), __builtin_amdgcn_fmed3f(v[1], -kMost, kMost)});
+        part[1][e] = take(v, v);
+        part[2][e] = take(v, v);
+    }
+    hi = __builtin_bit_cast(bf16x8, part[0]);
+    mid = __builtin_bit_cast(bf16x8, part[1]);
+    lo = __builtin_bit_cast(bf16x8, part[2]);
 }
 
 template <typename T>

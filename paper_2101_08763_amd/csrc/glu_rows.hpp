@@ -43,14 +43,10 @@ template <typename T>
 __device__ __forceinline__ RowsFrag<T> rows_frag(typename Chunk<T>::vec v) {
     RowsFrag<T> r;
     if constexpr (sizeof(T) == 4) {
+        f32x8 f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            __bf16 h, m, l;
-            split_parts(v[e], h, m, l);
-            r.part[0][e] = h;
-            r.part[1][e] = m;
-            r.part[2][e] = l;
-        }
+        for (int e = 0; e < 8; ++e) f[e] = v[e];
+        split_parts(f, r.part[0], r.part[1], r.part[2]);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) r.part[0][e] = v[e];
@@ -179,21 +175,24 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) r.x[j] = chunk(x[0], b, j, full);
     };
+    // 32 coordinates of weights of type T.
+    auto step = [&](auto weights, auto rows) {
+        RowsFrag<T> wf[TILES];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) wf[t] = weights(t);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const RowsFrag<T> xf = rows(m);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) acc[t][m] = rows_mma<T>(wf[t], xf, acc[t][m]);
+        }
+    };
     auto use = [&](const Block &r, int b, auto full) {
         auto x_frag = [&](int m, int j) { return rows_frag<T>(HOLD ? r.x[j] : chunk(x[m], b, j, full)); };
         if constexpr (GROUP == 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                RowsFrag<T> wf[TILES];
-#pragma unroll
-                for (int t = 0; t < TILES; ++t) wf[t] = rows_frag<T>(r.w[t][j]);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const RowsFrag<T> xf = x_frag(m, j);
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t) acc[t][m] = rows_mma<T>(wf[t], xf, acc[t][m]);
-                }
-            }
+            for (int j = 0; j < 4; ++j)
+                step([&](int t) { return rows_frag<T>(r.w[t][j]); }, [&](int m) { return x_frag(m, j); });
         } else {
             vec ones;
 #pragma unroll
@@ -244,9 +243,17 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
         }
     }
     if (whole < blocks && whole % kRowsWaves == wave) {
-        Block r;
-        load(r, whole, std::false_type());
-        use(r, whole, std::false_type());
+        if constexpr (GROUP == 0) {  // a loop: few instructions to bring to the CU for a part of a block
+#pragma unroll 1
+            for (int j = 0; whole * kW4Block + 32 * j < d; ++j) {
+                auto part = [&](const T *row) { return rows_frag<T>(chunk(row, whole, j, std::false_type())); };
+                step([&](int t) { return part(w[t]); }, [&](int m) { return part(x[m]); });
+            }
+        } else {
+            Block r;
+            load(r, whole, std::false_type());
+            use(r, whole, std::false_type());
+        }
     }
 
     // The wavefronts' sums, PASS units of a tile and 16 rows at a time, each added

@@ -535,12 +535,12 @@ hipError_t dense_launch(DenseLaunch a, hipStream_t st) {
 struct DenseChoice {
     bool large;
     int splits;
+    double us;
 };
 inline DenseChoice dense_choice(int64_t M, int64_t N, int64_t pairs, int64_t stages, bool glu, bool may_split) {
     const double cus = (double)std::max<int64_t>(1, device_cu_count());
     const int64_t half = glu ? 2 : 1;
-    DenseChoice best{false, 1};
-    double least = 0.0;
+    DenseChoice best{false, 1, 0.0};
     for (const bool large : {false, true}) {
         const int64_t bm = large ? LargeTile::BM : SmallTile::BM, bn = (large ? LargeTile::BN : SmallTile::BN) / half;
         const double tiles = (double)(((M + bm - 1) / bm) * ((N + bn - 1) / bn) * pairs);
@@ -549,7 +549,7 @@ inline DenseChoice dense_choice(int64_t M, int64_t N, int64_t pairs, int64_t sta
             const double each = (double)((stages + s - 1) / s);
             double t = std::max(1.0, std::ceil(tiles * (double)s / cus)) * (large ? 1.4 * each + 6.0 : 0.45 * each + 3.0);
             if (s > 1) t += 4.0 + 2.2e-6 * (double)(s * pairs * M * N);
-            if (least == 0.0 || t < least) least = t, best = {large, (int)s};
+            if (best.us == 0.0 || t < best.us) best = {large, (int)s, t};
         }
     }
     return best;

@@ -948,9 +948,9 @@ int stage_jobs(const Pieces &t, std::initializer_list<const StagedRows *> rows, 
 }
 
 int run_glu(const GluArgs &a, int prec, hipStream_t st) {
-    if (glu_takes_rows(prec, a.n, a.d, a.f)) return status_of(launch_glu_rows(prec, a, st));
     Pieces t;
     const StagedRows x(prec, a.x, a.n, a.d, &t), wg(prec, a.wg, a.f, a.d, &t), wu(prec, a.wu, a.f, a.d, &t);
+    if (glu_takes_rows(prec, a.n, a.d, a.f, t.bytes > 0)) return status_of(launch_glu_rows(prec, a, st));
     Scratch ws;
     if (t.bytes) {
         const int rc = alloc_uncaptured(&ws, t.bytes, workspace_limit(), st);

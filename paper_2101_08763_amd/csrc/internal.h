@@ -294,8 +294,10 @@ struct GluArgs {
     void *h, *g, *u;
 };
 // Few rows: the weights straight from memory, in any alignment; no temporary
-// memory.
-bool glu_takes_rows(int prec, int64_t n, int64_t d, int64_t f);
+// memory.  `staged`: the tiles' operands would have to be laid out first.
+bool glu_takes_rows(int prec, int64_t n, int64_t d, int64_t f, bool staged);
+// What the tiles are estimated to take, in us.
+double glu_tiles_us(int prec, int64_t n, int64_t d, int64_t f, bool staged);
 hipError_t launch_glu_rows(int prec, const GluArgs &a, hipStream_t st);
 
 // Weights of 4 bits: y = x W' + b, or the block on two of them (wu not null).

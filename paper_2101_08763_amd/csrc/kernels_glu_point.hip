@@ -16,13 +16,11 @@ __device__ __forceinline__ void store_operand(typename Operand<T>::E *p, int64_t
     using E = typename Operand<T>::E;
     typedef E vec __attribute__((ext_vector_type(8)));
     if constexpr (sizeof(T) == 4) {
-        vec h, m, l;
+        f32x8 f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            __bf16 a, b, c;
-            split_parts(v[i], a, b, c);
-            h[i] = a, m[i] = b, l[i] = c;
-        }
+        for (int i = 0; i < 8; ++i) f[i] = v[i];
+        bf16x8 h, m, l;
+        split_parts(f, h, m, l);
         *reinterpret_cast<vec *>(p) = h;
         *reinterpret_cast<vec *>(p + plane) = m;
         *reinterpret_cast<vec *>(p + 2 * plane) = l;

@@ -2,7 +2,6 @@
 // kernels (instantiated in kernels_w4_*.hip, one per type of the rows).
 #pragma once
 
-#include <cmath>
 
 #include "w4_tile.hpp"
 
@@ -10,22 +9,28 @@ namespace exemcl {
 
 template <typename T, int GROUP, bool GLU>
 hipError_t w4_sized(const RowsArgs &r, hipStream_t st) {
-    // Two blocks ahead pay where a block is few registers (us, one row, bf16, 1 / 2 / 4
-    // ahead: 8192 x 4096 by groups of 128 8.8 / 7.8 / 8.2, 1536 x 8192 by 32 4.6 / 5.0 /
-    // 8.0); 16 wavefronts to a workgroup spill.
-    if (r.n <= 16) return rows_launch<T, GROUP, GLU, 1, 1, (GROUP >= 64 ? 2 : 1)>(r, st);
-    if (r.n <= 32) return rows_launch<T, GROUP, GLU, 1, 2, 1>(r, st);
-    // Many rows: 64 at a time with the weights read again (from the caches), or tiles of
-    // 128 (fp32: 64) through LDS, whichever is estimated to take less (us, with one and
-    // the other, bf16 by groups of 128: 128 x 4096 x 8192 38 / 63, 256 73 / 64, 512 142 / 66;
-    // by 64: 256 x 1536 x 1536 10 / 34, 1000 28 / 35; fp32: 256 x 4096 x 4096 101 / 99).
     using P = W4TilePlan<T, GROUP>;
-    const double mats = GLU ? 2.0 : 1.0, cus = (double)std::max<int64_t>(1, device_cu_count());
-    const double rows = (double)((r.n + 63) / 64) * (double)r.f * (double)r.d * mats * (sizeof(T) == 4 ? 1.45e-6 : 6e-7);
-    const double workgroups = (double)((r.n + P::ROWS - 1) / P::ROWS) * (double)((r.f * (GLU ? 2 : 1) + 255) / 256);
+    // Rows at a time with the weights read again (from the caches), or tiles of 128 (fp32:
+    // 64) through LDS, whichever is estimated to take less (us, with one and the other,
+    // bf16 by groups of 128: 128 x 4096 x 8192 35 / 64, 256 70 / 64; two matrices, 512 x 512 x
+    // 2048 18 / 15; by groups of 64: 256 x 1536 x 1536 10 / 34; fp32: 128 x 4096 x 4096 39 / 84).
+    const int64_t cus = std::max<int64_t>(1, device_cu_count()), mats = GLU ? 2 : 1, pairs = (r.f + 31) / 32;
+    const double rows = 4.0 + (double)((r.n + 31) / 32 * mats) * (double)r.f * (double)r.d *
+                                  (sizeof(T) == 4 ? 5.6e-7 : GROUP == 32 ? 3.1e-7 : 2.5e-7);
+    const int64_t workgroups = (r.n + P::ROWS - 1) / P::ROWS * ((r.f * mats + 255) / 256);
     const double each = sizeof(T) == 4 ? 3.0 : GROUP == 128 ? 2.0 : GROUP == 64 ? 2.6 : 3.2;
-    if (rows <= std::ceil(workgroups / cus) * (double)w4_blocks(r.d) * each)
-        return rows_launch<T, GROUP, GLU, GLU ? 1 : 2, 4, 1>(r, st);
+    if (rows <= (double)((workgroups + cus - 1) / cus * w4_blocks(r.d)) * each) {
+        // 32 rows and two tiles of weights to a workgroup read least; with fewer results
+        // 16 rows, or one tile, where two blocks ahead pay (us, 16 rows and one tile / 16
+        // and two / 32 and two, bf16 by groups of 128: 16 x 4096 x 8192 11.2 / 7.9 / -,
+        // 16 x 8192 x 4096 10.8 / 11.6 / -, 64 x 4096 x 8192 35 / 21 / 20, 64 x 4096 x 2048
+        // 11.2 / 9.1 / 11.4, 64 x 8192 x 1024 11.8 / 12.0 / 19; fp32, two matrices by 64:
+        // 32 x 4096 x 8192 48 / 28 / 27).
+        auto fills = [&](int64_t n) { return 10 * pairs * ((r.n + n - 1) / n) >= 7 * cus; };
+        if (r.n > 16 && fills(32)) return rows_launch<T, GROUP, GLU, 2, 2, 1>(r, st);
+        if (fills(16)) return rows_launch<T, GROUP, GLU, 2, 1, 1>(r, st);
+        return rows_launch<T, GROUP, GLU, 1, 1, (GROUP >= 64 ? 2 : 1)>(r, st);
+    }
     return w4_tile_launch<T, GROUP, GLU>(r, st);
 }
 

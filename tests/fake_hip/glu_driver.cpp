@@ -34,8 +34,8 @@ static void check_capture() {
         fake::allocs.clear();
         fake::capture = hipStreamCaptureStatusActive;
         expect(grad(500, 300, 200, EXEMCL_BF16, 0, true, st) == EXEMCL_EINVAL, "gradient refuses", at);
-        expect(glu(500, 300, 200, EXEMCL_BF16, st) == EXEMCL_EINVAL, "rows to lay out", at);
-        expect(glu(500, 304, 200, EXEMCL_FP32, st) == EXEMCL_EINVAL, "parts to lay out", at);
+        expect(glu(2000, 300, 2000, EXEMCL_BF16, st) == EXEMCL_EINVAL, "rows to lay out", at);
+        expect(glu(2000, 304, 2000, EXEMCL_FP32, st) == EXEMCL_EINVAL, "parts to lay out", at);
         expect(fake::launches.empty() && fake::allocs.empty(), "nothing queued", at);
         expect(glu(500, 304, 200, EXEMCL_FP16, st) == EXEMCL_OK, "whole rows", at);
         expect(glu(64, 301, 200, EXEMCL_FP32, st) == EXEMCL_OK && glu(1, 301, 200, EXEMCL_BF16, st) == EXEMCL_OK, "few rows", at);

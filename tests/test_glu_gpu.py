@@ -410,7 +410,7 @@ def test_captured_and_replayed():
     many = randn(r, 300, d).to(t)
     q, _ = weights(r, f, d, 64)
     down, _ = weights(r, d, f, 32)
-    odd = randn(r, 300, 33).to(t), randn(r, f, 33).to(t)
+    odd = randn(r, 2000, 333).to(t), randn(r, 2000, 333).to(t)
 
     def calls():
         h, g, u = api.exemplar_glu(x, Wg, Wu, bg, bu, save=True)
