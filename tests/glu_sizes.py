@@ -17,3 +17,5 @@ W4 = [(1, 1, 1), (1, 40, 300), (1, 1301, 77), (3, 129, 33), (7, 2000, 15), (16, 
 # Enough rows for tiles through LDS: several blocks of 128 coordinates and one of less,
 # one block, one coordinate.
 W4_LARGE = [(2900, 700, 1500), (2500, 520, 150), (3000, 100, 700), (6000, 1, 40)]
+# Rows (n, d) whose values in each type fill half the last-level cache.
+W4_BACK = (16_500, 4101)

@@ -306,6 +306,21 @@ def test_w4_quantize_and_back(n, d, t, group):
         assert torch.equal(got[ok], want[ok].float().to(back)[()])
 
 
+@pytest.mark.parametrize("t", TYPES, ids=str)
+def test_w4_back_of_many_rows(t):
+    """Values past the last-level cache are those of the same rows in small calls (which
+    test_w4_quantize_and_back has against its reference)."""
+    n, d = glu_sizes.W4_BACK
+    q = api.exemplar_w4_quantize(randn(gen("back", str(t)), n, d).to(t), 32)
+    flat, out = inside((n, d), t, 1)
+    got = api.exemplar_w4_dequantize(q, t, out=out)
+    assert untouched(flat, 1)
+    for tile in (0, 517, q.codes.shape[0] - 8):
+        rows = min(128, n - 16 * tile)
+        some = api.W4Rows(q.codes[tile:tile + 8], q.words[tile:tile + 8], rows, d, 32)
+        assert torch.equal(got[16 * tile:16 * tile + rows], api.exemplar_w4_dequantize(some, t))
+
+
 def w4_bounds(x, W, q, bias, t):
     """The sum runs on q and z apart, each up to 15 s |x|: their magnitudes' sum, and
     two more steps for each group."""

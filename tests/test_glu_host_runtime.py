@@ -66,6 +66,7 @@ def test_sizes_of_the_tests_take_every_kernel(driver):
     calls += [("grad", *s, p, 0) for s in glu_sizes.LARGE for p in precs]
     calls += [(op, *s, p, g) for op in ("w4", "w4_glu") for s in glu_sizes.W4 + glu_sizes.W4_LARGE for p in precs for g in groups]
     calls += [(op, 70, 1000, 0, p, g) for op in ("quantize", "dequantize") for p in precs for g in groups]
+    calls += [("dequantize", *glu_sizes.W4_BACK, 0, p, 32) for p in precs]
     calls += [("empty", 0, 8, 6, 0, 0)]
     found = set().union(*(names(line) for line in launched(driver, calls)))
     every = names(run(driver, "all").stdout)
