@@ -147,7 +147,10 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[t][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const int blocks = (int)w4_blocks(d), whole = (int)(d / kW4Block);
+    // Whole blocks; weights of type T in steps of 32 coordinates where these are fewer
+    // than the wavefronts.
+    const int blocks = (int)w4_blocks(d), full_blocks = (int)(d / kW4Block);
+    const int whole = GROUP == 0 && full_blocks < kRowsWaves ? 0 : full_blocks;
     // A block as it comes from memory: the weights and their words, and x (many rows
     // of which are read when they are needed).
     constexpr bool HOLD = MT == 1;
@@ -245,18 +248,16 @@ __global__ __launch_bounds__(kRowsWaves * 64) void rows_kernel(const RowsArgs a)
             if (i == 0 || b0 + i * kRowsWaves < whole) use(r[i], b0 + i * kRowsWaves, std::true_type());
         }
     }
-    if (whole < blocks && whole % kRowsWaves == wave) {
-        if constexpr (GROUP == 0) {  // a loop: few instructions to bring to the CU for a part of a block
+    if constexpr (GROUP == 0) {
 #pragma unroll 1
-            for (int j = 0; whole * kW4Block + 32 * j < d; ++j) {
-                auto part = [&](const T *row) { return rows_frag<T>(chunk(row, whole, j, std::false_type())); };
-                step([&](int t) { return part(w[t]); }, [&](int m) { return part(x[m]); });
-            }
-        } else {
-            Block r;
-            load(r, whole, std::false_type());
-            use(r, whole, std::false_type());
+        for (int j = wave; whole * kW4Block + 32 * j < d; j += kRowsWaves) {
+            auto part = [&](const T *row) { return rows_frag<T>(chunk(row, whole, j, std::false_type())); };
+            step([&](int t) { return part(w[t]); }, [&](int m) { return part(x[m]); });
         }
+    } else if (whole < blocks && whole % kRowsWaves == wave) {
+        Block r;
+        load(r, whole, std::false_type());
+        use(r, whole, std::false_type());
     }
 
     // The wavefronts' sums, PASS units of a tile and 16 rows at a time, each added

@@ -20,9 +20,12 @@ namespace {
 //   fp32  16 x 4096 x 4096   28 / 39 / 58    30 / 41 / 53
 //         64 x 1024 x 2048   18 / 14 / 18    17 / 12 / 17
 //         128 x 4096 x 4096  195 / 144 / 111 191 / 135 / 102
+//         333 x 301 x 1111   25 / 18 / 15    21 / 15 / 15
+// Rows that begin at odd multiples of 2 bytes load at 2/5 of the rate (bf16 64 x 1001 x
+// 3000 17, 64 x 1000 x 3000 10).
 // Tiles of the dense kernels (glu_tile.hpp) take 41 us for 32 x 4096 x 8192 and 40
 // for 100 of bf16 (rows: 37 and 90), 219 for 128 x 4096 x 4096 of fp32 and 24 for
-// 333 x 301 x 1111 (rows: 17).
+// 333 x 301 x 1111 (rows: 15).
 struct Choice {
     int mt;
     double us;
@@ -31,13 +34,16 @@ Choice choose(int prec, int64_t n, int64_t d, int64_t f) {
     const bool wide = prec == P_FP32;
     constexpr double kBlock[2][3] = {{2.6, 3.6, 5.4}, {5.6, 8.4, 13.0}};
     const double cus = (double)std::max<int64_t>(1, device_cu_count()), blocks = (double)w4_blocks(d);
+    // The longest share of a wavefront: blocks, or steps of 32 where blocks are few.
+    const double longest = d / kW4Block < kRowsWaves ? std::ceil((double)((d + 31) / 32) / kRowsWaves) / 4.0 : std::ceil(blocks / kRowsWaves);
+    const double odd = !wide && d % 2 ? 2.5 : 1.0;
     const double bytes = (double)f * (double)d * (wide ? 8.0 : 4.0);
     Choice best{1, 0.0};
     for (int i = 0; i < 3; ++i) {
         const int mt = 1 << i;
         const double workgroups = (double)((f + 15) / 16) * (double)((n + 16 * mt - 1) / (16 * mt)) / cus;
-        const double turns = std::max(std::ceil(blocks / kRowsWaves), workgroups * blocks / kRowsWaves);
-        const double us = std::max(4.0 + turns * kBlock[wide][i] + workgroups * (wide ? 1.5 : 0.5), 3.0 + bytes / 4.6e6);
+        const double turns = std::max(longest, workgroups * blocks / kRowsWaves);
+        const double us = std::max(4.0 + turns * kBlock[wide][i] * odd + workgroups * (wide ? 1.5 : 0.5), 3.0 + bytes / 4.6e6);
         if (best.us == 0.0 || us < best.us) best = {mt, us};
     }
     return best;

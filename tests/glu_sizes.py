@@ -7,7 +7,7 @@ them)."""
 # coordinate, one result.
 GLU = [(1, 1, 1), (1, 40, 300), (1, 301, 77), (2, 129, 33), (5, 1000, 16), (16, 128, 130), (17, 64, 257), (33, 7, 19),
        (64, 520, 100), (65, 520, 100), (100, 33, 129), (257, 301, 300), (300, 1, 5), (130, 256, 1), (1000, 100, 511),
-       (60, 1001, 2041)]
+       (60, 1001, 2041), (700, 130, 1300)]
 # Enough tiles for the largest: of h, of dx, of dw.
 LARGE = [(4100, 40, 2060), (4100, 2090, 130), (130, 1300, 2900)]
 
