@@ -428,8 +428,8 @@ EXEMCL_API int exemplar_mx_eval(const void *codes, const void *scales, int64_t n
  * may be NULL), and infinities and NaN go the way of arithmetic (of fp32 rows and
  * weights in exemplar_glu and its gradient an infinity may come out as NaN).  Outputs
  * must not overlap inputs.  All sums are in fp32 or wider, in an order that the
- * sizes decide (and for the gradient the memory that is to be had): results are
- * bitwise reproducible.
+ * sizes and the arrays' alignment decide (and for the gradient the memory that is to
+ * be had): results are bitwise reproducible.
  *
  * Temporary memory, taken as exemplar_eval does: exemplar_glu_backward always (n > 0,
  * f > 0) and exemplar_glu, of more than 64 rows, where x, Wg or Wu has to be laid out
