@@ -15,9 +15,12 @@
 // 2 048 x 4 096 x 8 192 of bf16 by groups of 128 take 147 us, 0.93 PFLOP/s, the matrix
 // cores busy 46 % of the cycles; by 64 and 32 it takes 5 and 34 % more (twice and four
 // times the scales and zero points), of fp32 2.2 times as long (three parts).  Leaving
-// out the FMAs, or the staging of x, would save a fifth each.  VALU and matrix phases
-// held apart by barriers took 9 % more, and hints to the compiler's scheduling changed
-// nothing.
+// out the FMAs, or the staging of x, would save a fifth each.  The VALU is busy 53 %,
+// and a wavefront waits for 30 % of its time: behind the barrier all read their next x
+// together.  Registers for it twice, or a third wavefront to a SIMD, do not fit (251
+// are in use).  VALU and matrix phases held apart by barriers took 9 % more, and a
+// higher priority for half of the wavefronts or hints to the compiler's scheduling
+// changed nothing.
 #pragma once
 
 #include <atomic>
