@@ -532,7 +532,8 @@ EXEMCL_API int exemplar_w4_dequantize(const void *codes, const uint32_t *words, 
  * rounded further) and weights of f rows of 4 bits; y is n x f of x's type, bias f
  * floats or NULL.  A group's products are added with whole q, and s and z applied to
  * the sum, in fp32 (fp32 rows in three bf16 parts, all of each; an infinity in x may
- * come out as NaN).  No temporary memory.
+ * come out as NaN, and so may values past 2^112, whose sums with whole q and z end
+ * before s makes them smaller).  No temporary memory.
  */
 EXEMCL_API int exemplar_w4_product(const void *x, int64_t n, int64_t d, int precision, const void *codes,
                                    const uint32_t *words, int64_t f, int group, const float *bias, void *y, void *stream);

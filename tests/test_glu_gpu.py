@@ -189,6 +189,24 @@ def test_nan_stays_in_its_row_and_column(n, t):
         assert torch.equal(a.isnan(), nan) and torch.equal(a[~nan], b[~nan])
 
 
+@pytest.mark.parametrize("n,d,f", [(3, 70, 40), (700, 130, 1300)])
+def test_rows_at_the_end_of_fp32(n, d, f):
+    """Values that round to an infinity of the parts' type, or to its largest number,
+    are whole in three parts: the bounds of any others hold."""
+    r = gen("end", n)
+    x, Wg, Wu, _, _ = block(r, n, d, f, torch.float32, False)
+    x = x * 2.0 ** 123
+    top = torch.finfo(torch.float32).max
+    x[0, :6] = torch.tensor([top, -top, float.fromhex("0x1.fefffep127"), float.fromhex("0x1.ffp127"),
+                             float.fromhex("-0x1.fep127"), float.fromhex("0x1.feffffp127")])
+    Wg, Wu = Wg * 2.0 ** -90, Wu * 2.0 ** -90
+    assert bool(x.isfinite().all())
+    got = api.exemplar_glu(x, Wg, Wu, activation=api.EXEMCL_RELU, save=True)
+    want = ref.glu(x.double(), Wg.double(), Wu.double(), None, None, "relu")
+    for a, b, e, name in zip(got, want, ref.glu_bounds(x.double(), Wg.double(), Wu.double(), None, None, "relu", torch.float32), "hgu"):
+        close(a, b, e, name)
+
+
 @pytest.mark.parametrize("act", ref.ACTIVATIONS)
 @pytest.mark.parametrize("t", TYPES, ids=str)
 def test_activations_far_out(act, t):
