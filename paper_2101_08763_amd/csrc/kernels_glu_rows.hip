@@ -20,7 +20,7 @@ namespace {
 //   fp32  16 x 4096 x 4096   28 / 39 / 58    30 / 41 / 53
 //         64 x 1024 x 2048   18 / 14 / 18    17 / 12 / 17
 //         128 x 4096 x 4096  195 / 144 / 111 191 / 135 / 102
-//         333 x 301 x 1111   25 / 18 / 15    21 / 15 / 15
+//         333 x 301 x 1111   25 / 21 / 16    21 / 15 / 15
 // Rows that begin at odd multiples of 2 bytes load at 2/5 of the rate (bf16 64 x 1001 x
 // 3000 17, 64 x 1000 x 3000 10).
 // Tiles of the dense kernels (glu_tile.hpp) take 41 us for 32 x 4096 x 8192 and 40
@@ -42,7 +42,9 @@ Choice choose(int prec, int64_t n, int64_t d, int64_t f) {
     for (int i = 0; i < 3; ++i) {
         const int mt = 1 << i;
         const double workgroups = (double)((f + 15) / 16) * (double)((n + 16 * mt - 1) / (16 * mt)) / cus;
-        const double turns = std::max(longest, workgroups * blocks / kRowsWaves);
+        // (of fp32 one workgroup is on a CU at a time)
+        const double rounds = wide && workgroups > 1.0 ? std::ceil(workgroups) : workgroups;
+        const double turns = std::max(longest, rounds * blocks / kRowsWaves);
         const double us = std::max(4.0 + turns * kBlock[wide][i] * odd + workgroups * (wide ? 1.5 : 0.5), 3.0 + bytes / 4.6e6);
         if (best.us == 0.0 || us < best.us) best = {mt, us};
     }
