@@ -173,7 +173,9 @@ hipError_t launch_dense_stage(int prec, const DenseStageJob *jobs, int count, hi
     return prec == P_FP32 ? stage<float>(jobs, count, st) : stage<uint16_t>(jobs, count, st);
 }
 
-// Enough workgroups for the chip, of 64 rows and more where there are many.
+// Enough workgroups for the chip, of 64 rows and more where there are many (us with
+// the column sums, mean of 8 192 x 4 096, 16 384 x 8 192 and 2 000 x 512 of bf16: 1 024
+// workgroups 107, 2 048 110, 4 096 103, 16 384 104).
 int64_t glu_point_parts(int64_t n, int64_t f) {
     const int64_t cb = (dense_ld(f) / 8 + kPointCols - 1) / kPointCols;
     const int64_t most = std::min<int64_t>((n + kPointRows - 1) / kPointRows, 512);
