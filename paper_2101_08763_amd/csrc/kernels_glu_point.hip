@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "glu_device.hpp"
+#include "glu_stage.hpp"
 #include "mfma_kernels.hpp"
 
 namespace exemcl {
@@ -33,30 +34,24 @@ __device__ __forceinline__ void store_operand(typename Operand<T>::E *p, int64_t
 }
 
 // Rows as operands; T: float, or uint16_t for either 16-bit type.
-struct StageJobs {
-    DenseStageJob job[3];
-    int64_t blocks[3];  // workgroups up to and with each
-};
 template <typename T>
 __device__ __forceinline__ void stage_rows(const StageJobs &jobs, int64_t b) {
-    const int which = b < jobs.blocks[0] ? 0 : b < jobs.blocks[1] ? 1 : 2;
-    if (which) b -= jobs.blocks[which - 1];
-    const DenseStageJob j = jobs.job[which];
-    const int64_t ld = (j.d + 7) / 8 * 8, per = ld / 8, i = b * 256 + threadIdx.x, row = i / per, c = i - row * per;
-    if (row >= j.n) return;
-    const T *src = (const T *)j.src + row * j.d + c * 8;
-    const int have = (int)min((int64_t)8, j.d - c * 8);
+    const StagePlace at = stage_place(jobs, b, threadIdx.x);
+    if (at.job < 0) return;
+    const DenseStageJob j = jobs.job[at.job];
+    const T *src = (const T *)j.src + at.row * j.d + at.c;
+    const int have = (int)min((int64_t)8, j.d - at.c);
     if constexpr (sizeof(T) == 4) {
         float v[8];
         load8(src, have, v);
-        store_operand<T>((__bf16 *)j.dst + row * ld + c * 8, j.n * ld, v);
+        store_operand<T>((__bf16 *)j.dst + at.row * at.ld + at.c, j.n * at.ld, v);
     } else {
         typedef T vec __attribute__((ext_vector_type(8)));
-        *reinterpret_cast<vec *>((T *)j.dst + row * ld + c * 8) = load8(src, have);
+        *reinterpret_cast<vec *>((T *)j.dst + at.row * at.ld + at.c) = load8(src, have);
     }
 }
 template <typename T>
-__global__ __launch_bounds__(256) void dense_stage_kernel(const StageJobs jobs) {
+__global__ __launch_bounds__(kStageThreads) void dense_stage_kernel(const StageJobs jobs) {
     stage_rows<T>(jobs, flat_block());
 }
 
@@ -71,6 +66,7 @@ __global__ __launch_bounds__(256) void zero_bytes_kernel(uint16_t *__restrict__ 
 // the type of the products' operands (fp32: three parts, all of it); the column
 // sums are of what is rounded, in fp32 within a part.
 constexpr int kPointCols = 32, kPointRows = 8;
+static_assert(kPointCols * kPointRows == kStageThreads, "both kinds of workgroups in one launch");
 template <typename T, int ACT>
 __global__ __launch_bounds__(kPointCols *kPointRows) void glu_point_kernel(
     const T *__restrict__ dh, const T *__restrict__ gate, const T *__restrict__ up, int64_t n, int64_t f, int64_t ld,
@@ -117,19 +113,6 @@ __global__ __launch_bounds__(kPointCols *kPointRows) void glu_point_kernel(
     }
 }
 
-// The jobs' workgroups; returns their number.
-int64_t stage_jobs(const DenseStageJob *jobs, int count, StageJobs *s) {
-    int64_t blocks = 0;
-    for (int i = 0; i < 3; ++i) {
-        if (i < count) {
-            s->job[i] = jobs[i];
-            blocks += (jobs[i].n * (dense_ld(jobs[i].d) / 8) + 255) / 256;
-        }
-        s->blocks[i] = blocks;
-    }
-    return blocks;
-}
-
 template <typename T>
 hipError_t point(const GluPointArgs &a, hipStream_t st) {
     using E = typename Operand<T>::E;
@@ -159,7 +142,7 @@ hipError_t stage(const DenseStageJob *jobs, int count, hipStream_t st) {
     const int64_t blocks = stage_jobs(jobs, count, &s);
     if (blocks > int64_t(1) << 34) return hipErrorInvalidValue;
     if (blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL(dense_stage_kernel<T>, flat_grid(blocks, 256), dim3(256), 0, st, s);
+    hipLaunchKernelGGL(dense_stage_kernel<T>, flat_grid(blocks, kStageThreads), dim3(kStageThreads), 0, st, s);
     return hipGetLastError();
 }
 
