@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from types import SimpleNamespace
 from typing import Any, NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -405,26 +406,35 @@ def _mx_empty(n, d, format, device, empty):
 
 
 def _check_gradient(name, tensors):
-    """Results carry no autograd graph: a gradient that is asked for would be lost
+    """Results carry no autograd graph and no tangent: a gradient that is asked for, or
+    a forward-mode derivative (which torch.no_grad() does not switch off), would be lost
     without a word.  (Codes of rows have none to lose.)"""
     import torch
-    if name not in ("exemplar_mx_quantize", "exemplar_w4_quantize") and torch.is_grad_enabled() \
-            and any(t is not None and t.requires_grad for t in tensors):
+    if name in ("exemplar_mx_quantize", "exemplar_w4_quantize"):
+        return
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
         raise ValueError(f"{name} records no gradient: call it under torch.no_grad() or on detached tensors "
                          "(exemplar_rmsnorm_backward computes the norm's, exemplar_glu_backward the gated block's)")
+    unpack = torch.autograd.forward_ad.unpack_dual
+    if any(t is not None and unpack(t).tangent is not None for t in tensors):
+        raise ValueError(f"{name} records no forward-mode derivative: call it on the primals "
+                         "(torch.autograd.forward_ad.unpack_dual)")
 
 
-_DEVICE_QUERIES = None  # (current device, its current raw stream), where PyTorch has them
+_QUERIES = None  # (current device, its current raw stream, forward_ad), where PyTorch has them
 
 
-def _device_queries():
-    global _DEVICE_QUERIES
-    if _DEVICE_QUERIES is None:
+def _queries():
+    global _QUERIES
+    if _QUERIES is None:
         import torch
-        _DEVICE_QUERIES = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
-                           getattr(torch._C, "_cuda_getCurrentRawStream",
-                                   lambda dev: torch.cuda.current_stream(dev).cuda_stream))
-    return _DEVICE_QUERIES
+        from torch.autograd import forward_ad
+        _QUERIES = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
+                    getattr(torch._C, "_cuda_getCurrentRawStream",
+                            lambda dev: torch.cuda.current_stream(dev).cuda_stream),
+                    # (tangents are there only inside a level; without its number always looked for)
+                    forward_ad if hasattr(forward_ad, "_current_level") else SimpleNamespace(_current_level=0))
+    return _QUERIES
 
 
 def _run(name, tensors, stream, *args):
@@ -432,13 +442,15 @@ def _run(name, tensors, stream, *args):
     one's; None: not given) with ``args`` and the stream, and raise its error.
     The checks and messages are _check_device's; the calls on rows can be a few
     microseconds each, so the common case takes the short way."""
+    current_device, raw_stream, forward_ad = _QUERIES or _queries()
+    if forward_ad._current_level >= 0:
+        _check_gradient(name, tensors)
     dev = tensors[0].get_device()
     for t in tensors:
         if t is not None and (t.get_device() != dev or not t.is_contiguous() or t.requires_grad or dev < 0):
             _check_gradient(name, tensors)
             _check_device(*tensors)
     fn = getattr(_LIB or load(), name)
-    current_device, raw_stream = _DEVICE_QUERIES or _device_queries()
     if dev == current_device():
         rc = fn(*args, raw_stream(dev) if stream is None else _stream(stream))
     else:
@@ -661,7 +673,7 @@ def exemplar_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, save=False
     weights of its type (f x d), biases in float32; g and u are kept for
     exemplar_glu_backward where ``save``, else None (see exemplar_glu in
     exemcl.h).  No autograd graph is recorded, and tensors that require a gradient
-    are refused outside torch.no_grad()."""
+    are refused outside torch.no_grad(), those with a tangent always."""
     if x.dim() != 2 or Wg.dim() != 2:
         raise ValueError("x must be n x d and Wg f x d")
     dtype = x.dtype
