@@ -17,7 +17,7 @@
 // times the scales and zero points), of fp32 2.2 times as long (three parts).  Leaving
 // out the FMAs, or the staging of x, would save a fifth each.  The VALU is busy 53 %,
 // and a wavefront waits for 30 % of its time: behind the barrier all read their next x
-// together.  Registers for it twice, or a third wavefront to a SIMD, do not fit (251
+// together.  Registers for it twice, or a third wavefront to a SIMD, do not fit (256
 // are in use).  VALU and matrix phases held apart by barriers took 9 % more, and a
 // higher priority for half of the wavefronts or hints to the compiler's scheduling
 // changed nothing.
@@ -39,8 +39,8 @@ struct W4TilePlan {
     static constexpr int SUMS = GPB > 4 / SPW ? GPB : 4 / SPW;        // partial sums of x in a block
     static constexpr int X = XT * 4 * PARTS * 1024;                   // bytes of a block's x
     static constexpr int XS = SUMS * ROWS * 4;                        // its sums
-    static constexpr int S = WN * RT * GPB * 64;                      // scales; minus scales times zero points
-    static constexpr int XS_AT = 2 * X, S_AT = XS_AT + 4 * XS, SZ_AT = S_AT + 4 * S, LDS = SZ_AT + 4 * S;
+    static constexpr int S = WN * RT * GPB * 64;                      // scales; minus zero points
+    static constexpr int XS_AT = 2 * X, S_AT = XS_AT + 4 * XS, Z_AT = S_AT + 4 * S, LDS = Z_AT + 4 * S;
     static_assert(LDS <= kLdsBytes, "geometry");
 };
 
@@ -110,8 +110,9 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
             xr[j] = load8(x + (uint32_t)(xrow_at + (full ? k : min(k, d - 1))), full ? 8 : d - k);
         }
     };
-    // The loaded block into LDS: x and its sums, the scales, and minus scale times
-    // zero point.
+    // The loaded block into LDS: x and its sums, the scales, and minus the zero points
+    // (a scale times its zero point may pass fp32's range where the sum that it is
+    // taken from does not).
     auto store = [&](int b) {
         unsigned char *to = smem + (b & 1) * P::X;
         vec ones;
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
             const float s = __uint_as_float(wr[i] & 0xffffff00u), z = (float)(wr[i] & 0xffu);
             const int at = (b & 3) * P::S + (wave * 2 + i) * GPB * 64 + word_at * 4;
             *reinterpret_cast<float *>(smem + P::S_AT + at) = s;
-            *reinterpret_cast<float *>(smem + P::SZ_AT + at) = -s * z;
+            *reinterpret_cast<float *>(smem + P::Z_AT + at) = -z;
         }
 #pragma unroll
         for (int q = 0; q < HERE; ++q) {
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
         }
     };
 
-    f32x4 acc[RT][MT], p[MT], sc = {0.0f, 0.0f, 0.0f, 0.0f}, sz = sc;
+    f32x4 acc[RT][MT], p[MT], sc = {0.0f, 0.0f, 0.0f, 0.0f}, zp = sc;
     float xs[MT];
     RowsFrag<T> xf[MT][STEPS];
     vec wf[STEPS];
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
         constexpr int nu = (u + 1) % UNITS, nt = nu % RT, nq = nu / RT, pt = (u + UNITS - 1) % UNITS % RT;
         if constexpr (u != 2) __builtin_amdgcn_sched_barrier(0);  // (the next block's stores go between the second's instructions)
         const int s_at = (b & 3) * P::S + ((wn * RT + t) * GPB + q) * 64 + g * 16;
-        const f32x4 s_now = *reinterpret_cast<const f32x4 *>(smem + P::S_AT + s_at), z_now = *reinterpret_cast<const f32x4 *>(smem + P::SZ_AT + s_at);
+        const f32x4 s_now = *reinterpret_cast<const f32x4 *>(smem + P::S_AT + s_at), z_now = *reinterpret_cast<const f32x4 *>(smem + P::Z_AT + s_at);
         float xs_now[MT];
         if constexpr (t == 0)
 #pragma unroll
@@ -184,7 +185,7 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
             for (int m = 0; m < MT; ++m) {
                 if (j == 0) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[pt][m][i] = fmaf(sz[i], xs[m], fmaf(sc[i], p[m][i], acc[pt][m][i]));
+                    for (int i = 0; i < 4; ++i) acc[pt][m][i] = fmaf(sc[i], fmaf(zp[i], xs[m], p[m][i]), acc[pt][m][i]);
                     p[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
                 }
                 p[m] = rows_mma_whole<T>(wf[j], xf[m][j], p[m]);
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
                 for (int m = 0; m < MT; ++m) xf[m][j] = read_x(u == UNITS - 1 ? b + 1 : b, m, (q + 1) % GPB * STEPS + j);
             wf[j] = w4_operand(c[nt][nq * STEPS + j], E());
         }
-        sc = s_now, sz = z_now;
+        sc = s_now, zp = z_now;
         if constexpr (t == 0)
 #pragma unroll
             for (int m = 0; m < MT; ++m) xs[m] = xs_now[m];
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(512, 2) void w4_tile_kernel(const RowsArgs a) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[RT - 1][m][i] = fmaf(sz[i], xs[m], fmaf(sc[i], p[m][i], acc[RT - 1][m][i]));
+        for (int i = 0; i < 4; ++i) acc[RT - 1][m][i] = fmaf(sc[i], fmaf(zp[i], xs[m], p[m][i]), acc[RT - 1][m][i]);
 
 #pragma unroll
     for (int t = 0; t < RT; t += MATS) {
