@@ -515,7 +515,9 @@ EXEMCL_API int exemplar_w4_layout(int64_t n, int64_t d, int group, int64_t *code
  * and largest value of a group and of 0, s = (hi - lo) / 15 rounded up to 16
  * significant bits (0 below 2^-126: the group counts as zeros), and with r the fp32
  * reciprocal of s, z = round(-lo r) and q = round(v r) + z, both within 0 .. 15,
- * ties to even.  A group that holds an infinity or a NaN is all NaN.
+ * ties to even.  A q whose value would be an infinity of w's type is one step nearer
+ * to z, so that finite weights stay finite.  A group that holds an infinity or a NaN is
+ * all NaN.
  *
  *   w             device, n x d row-major, type per `precision`
  *   codes, words  device; written, padding included

@@ -8,6 +8,14 @@ namespace exemcl {
 
 namespace {
 
+// The largest number of a type.
+template <typename T>
+constexpr float kLargest = 0x1.fffffep127f;
+template <>
+constexpr float kLargest<_Float16> = 65504.0f;
+template <>
+constexpr float kLargest<__bf16> = 0x1.fep127f;
+
 // A wavefront takes a tile of 16 rows x 128 coordinates: lane (r, q) row r and the
 // coordinates 32 j + 8 q + e, which are its 16 bytes.  A group's extremes are those
 // of the lanes q of a row, over the j that belong to it.  HBM-bound: 32 768 rows of
@@ -52,14 +60,23 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T *__restrict__ 
         const uint32_t sbits = bad ? 0x7fc00000u : s0 < 0x1p-126f ? 0u : (__float_as_uint(s0) + 255u) & ~255u;
         const float s = __uint_as_float(sbits), inv = s > 0.0f ? 1.0f / s : 0.0f;
         const float z = bad ? 0.0f : fminf(fmaxf(rintf(-lo * inv), 0.0f), 15.0f);
+        // Where a value of the group may round to an infinity, a code whose value does goes
+        // one step towards z: that is enough, it is half a step at most past its weight.
+        const bool far = s * 15.0f > kLargest<T>;
 #pragma unroll
         for (int j = p * STEPS; j < (p + 1) * STEPS; ++j) {
             uint32_t c = 0;
+            float t[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] = fminf(fmaxf(rintf(v[j][e] * inv) + z, 0.0f), 15.0f);
+            if (__builtin_amdgcn_ballot_w64(far) != 0)  // (a jump over it)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (__builtin_isinf(to_f32((T)((t[e] - z) * s)))) t[e] += t[e] > z ? -1.0f : 1.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int64_t k = b * kW4Block + 32 * j + 8 * q + e;
-                const float t = fminf(fmaxf(rintf(v[j][e] * inv) + z, 0.0f), 15.0f);
-                const uint32_t code = bad || row >= n || k >= d ? 0u : (uint32_t)t;
+                const uint32_t code = bad || row >= n || k >= d ? 0u : (uint32_t)t[e];
                 c |= code << (e % 4 * 8 + e / 4 * 4);
             }
             out[j] = c;
