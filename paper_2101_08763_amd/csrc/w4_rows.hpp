@@ -18,7 +18,12 @@ hipError_t w4_sized(const RowsArgs &r, hipStream_t st) {
     // 11.2 / 9.1 / 11.4, 64 x 8192 x 1024 11.8 / 12.0 / 19; fp32, two matrices by 64:
     // 32 x 4096 x 8192 48 / 28 / 27).
     auto fills = [&](int64_t n) { return 10 * pairs * ((r.n + n - 1) / n) >= 7 * cus; };
-    const int xt = r.n > 16 && fills(32) ? 2 : 1, wt = xt == 2 || fills(16) ? 2 : 1;
+    // The block by groups of 32 spills registers where a workgroup has two tiles (us, one
+    // tile / two): fp32 and 16 rows 36 of them, 83 / 133 for 1 x 4096 x 32768, and it takes one;
+    // 32 rows 38, 189 / 158 for 17; fp16 and bf16 8 and 19, 52 / 54 for 1, 62 / 58 for 16 and
+    // 115 / 103 for 32.
+    constexpr bool ONE = WIDE && GLU && GROUP == 32;
+    const int xt = r.n > 16 && fills(32) ? 2 : 1, wt = xt == 2 || (!ONE && fills(16)) ? 2 : 1;
     // Those, with the weights read again (from the caches) for every 16 xt rows, or tiles
     // of 128 rows (fp32: 64) through LDS, whichever is estimated to take less.  Few rows:
     // what the launch, the instructions for 16 rows and a workgroup's start and join take;
@@ -39,7 +44,8 @@ hipError_t w4_sized(const RowsArgs &r, hipStream_t st) {
     const double block = WIDE ? 2.9 : GROUP == 128 ? 2.2 : GROUP == 64 ? 2.4 : 3.2;
     if (rows > 3.0 + (double)rounds * ((double)w4_blocks(r.d) * block + 2.5)) return w4_tile_launch<T, GROUP, GLU>(r, st);
     if (xt == 2) return rows_launch<T, GROUP, GLU, 2, 2, 1>(r, st);
-    if (wt == 2) return rows_launch<T, GROUP, GLU, 2, 1, 1>(r, st);
+    if constexpr (!ONE)
+        if (wt == 2) return rows_launch<T, GROUP, GLU, 2, 1, 1>(r, st);
     return rows_launch<T, GROUP, GLU, 1, 1, (GROUP >= 64 ? 2 : 1)>(r, st);
 }
 

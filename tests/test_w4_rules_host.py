@@ -52,3 +52,10 @@ def test_sizes_of_the_range_tests(driver):  # noqa: F811
     calls = [(op, 2900, 700, 1500, p, g) for op in ("w4", "w4_glu") for p in (0, 2) for g in (32, 64, 128)]
     calls += [("w4", 6000, 40, 700, p, 32) for p in (0, 1, 2)]
     assert all("w4_tile" in line for line in launched(driver, calls))
+
+
+def test_blocks_by_groups_of_32(driver):  # noqa: F811
+    """Two tiles and 16 rows of fp32 spill registers: 133 us, one tile 83."""
+    one, = launched(driver, [("w4_glu", 1, 4096, 32768, 0, 32)])
+    two, = launched(driver, [("w4_glu", 1, 4096, 32768, 0, 64)])
+    assert "rows_kernelIfLi32ELb1ELi1ELi1E" in one and "rows_kernelIfLi64ELb1ELi2ELi1E" in two, (one, two)
