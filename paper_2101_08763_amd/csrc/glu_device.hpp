@@ -9,10 +9,11 @@
 namespace exemcl {
 
 // ---------------------------------------------------------------------------
-// Activations.  sigma(z) = 1 / (1 + e^-z); FAST (results of 16 bits): the
-// exponential and the reciprocal of the instructions, together within 2^-19 of
-// the value for |z| < 64 (the argument's own rounding, z log2 e 2^-24, is most of
-// it), against the 2^-12 at least of the result's type.
+// Activations.  sigma(z) = 1 / (1 + e^-z); FAST (results of 16 bits): the exponential
+// and the reciprocal of the instructions, together within (1.25 |z| + 5) 2^-24 of the
+// value, 2^-17.6 at |z| = 64 (the argument's own rounding and its constant's are most of
+// it; the six roundings that make gelu_tanh's z add 6 |z| 2^-24, 2^-15 there), against
+// the 2^-12 at least of the result's type.
 // ---------------------------------------------------------------------------
 template <bool FAST>
 __device__ __forceinline__ float sigma(float z) {
