@@ -456,7 +456,8 @@ enum exemcl_activation {
  *              rounded; either may be NULL (h is made from the unrounded values)
  *
  * Each result is rounded once.  fp32 products are those of three bf16 parts of each
- * value, six products for one, which leave out less than 2^-26 of it.
+ * value, six products for one, which leave out less than 2^-26 of it (of a value below
+ * 2^-110, here and in the calls below, up to 2^-134: bf16's last place ends there).
  */
 EXEMCL_API int exemplar_glu(const void *x, int64_t n, int64_t d, const void *Wg, const void *Wu, int64_t f,
                             const float *bg, const float *bu, int precision, int activation, void *h, void *g, void *u,

@@ -79,6 +79,7 @@ __device__ __forceinline__ void with_activation(int act, F &&f) {
 // in the fp32 accumulators: 2.7 times the fp32 instruction's rate.  A value that
 // would round to an infinity keeps the largest bf16 as its upper part.  Of an
 // infinity that leaves one, whose rest is NaN; a NaN is NaN from the second part on.
+// Parts count down to 2^-133, so that values below 2^-110 lose up to 2^-134.
 // ---------------------------------------------------------------------------
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ void split_parts(f32x8 x, bf16x8 &hi, bf16x8 &mid, bf16x8 &lo) {
