@@ -426,16 +426,18 @@ EXEMCL_API int exemplar_mx_eval(const void *codes, const void *scales, int64_t n
  * The conventions above (ownership, streams, asynchrony, dense row-major arrays)
  * hold, n and f may be 0 (nothing is queued where nothing is written, and the arrays
  * may be NULL), and infinities and NaN go the way of arithmetic (of fp32 rows and
- * weights in exemplar_glu and its gradient an infinity may come out as NaN).  Outputs
- * must not overlap inputs.  All sums are in fp32 or wider, in an order that the
- * sizes and the arrays' alignment decide (and for the gradient the memory that is to
- * be had): results are bitwise reproducible.
+ * weights in exemplar_glu and its gradient, and of rows in the calls on 4-bit weights, an
+ * infinity may come out as NaN).  Outputs must not overlap inputs.  All sums are in fp32
+ * or wider, in an order that the sizes and the arrays' alignment decide (and for the
+ * gradient whether both of dWg and dWu are asked for, and the memory that is to be had):
+ * results are bitwise reproducible.
  *
  * Temporary memory, taken as exemplar_eval does: exemplar_glu_backward always (n > 0,
  * f > 0) and exemplar_glu, of more than 64 rows, where x, Wg or Wu has to be laid out
  * again (fp32, d not a multiple of 8, an address not a multiple of 16 bytes) and the
- * sizes are better served that way.  On a capturing stream those calls return EINVAL
- * and queue nothing; the others may be captured.
+ * sizes are better served that way; never for up to 64 rows, nor of 16-bit types where d
+ * is a multiple of 8 and the three arrays are 16-byte aligned.  On a capturing stream
+ * calls that take some return EINVAL and queue nothing; the others may be captured.
  * ------------------------------------------------------------------------ */
 enum exemcl_activation {
     EXEMCL_SILU = 0,      /* g / (1 + e^-g) */
@@ -475,8 +477,9 @@ EXEMCL_API int exemplar_glu(const void *x, int64_t n, int64_t d, const void *Wg,
  *              floats.  Written; each may be NULL and is then not computed.  For
  *              n = 0 the sums are zeros.
  *
- * The products take dg and du rounded to the type (fp32: in three bf16 parts); the
- * sums dbg and dbu take them unrounded.  dx is one sum over both matrices.
+ * The products take dg and du rounded to the type (fp32: in three bf16 parts), so that
+ * of fp16 those past 65 504 are infinite there; the sums dbg and dbu take them
+ * unrounded.  dx is one sum over both matrices.
  * Temporary memory: dg and du (4 n f bytes; fp32: 12 n f), up to 4096 f bytes for the
  * sums, x, Wg and Wu where they have to be laid out again, and up to 1 GB of partial
  * sums of products with few results and long sums (the call does without where that is
@@ -534,9 +537,9 @@ EXEMCL_API int exemplar_w4_dequantize(const void *codes, const uint32_t *words, 
  * exemplar_w4_product -- y = x W' + bias for rows x (n x d, type per `precision`, not
  * rounded further) and weights of f rows of 4 bits; y is n x f of x's type, bias f
  * floats or NULL.  A group's products are added with whole q, and s and z applied to
- * the sum, in fp32 (fp32 rows in three bf16 parts, all of each; an infinity in x may
- * come out as NaN, and so may values past 2^112, whose sums with whole q and z end
- * before s makes them smaller).  No temporary memory.
+ * the sum, in fp32 (fp32 rows in three bf16 parts, all of each).  An infinity in x, of
+ * any type, may come out as NaN, and so may values past 2^112, whose sums with whole q
+ * and z end before s makes them smaller.  No temporary memory.
  */
 EXEMCL_API int exemplar_w4_product(const void *x, int64_t n, int64_t d, int precision, const void *codes,
                                    const uint32_t *words, int64_t f, int group, const float *bias, void *y, void *stream);

@@ -700,7 +700,8 @@ def exemplar_glu(x, Wg, Wu, bg=None, bu=None, activation=EXEMCL_SILU, save=False
 def exemplar_glu_backward(dh, x, Wg, Wu, g, u, activation=EXEMCL_SILU, bias=False, stream=None):
     """(dx, dWg, dWu, dbg, dbu) of exemplar_glu from the gradient dh of h and the g
     and u it returned: dx and the weights' in x's type, the biases' in float32, None
-    unless ``bias`` (see exemplar_glu_backward in exemcl.h)."""
+    unless ``bias`` (see exemplar_glu_backward in exemcl.h, where any may be left out:
+    here the first three are always computed)."""
     import torch
     if x.dim() != 2 or Wg.dim() != 2:
         raise ValueError("x must be n x d and Wg f x d")

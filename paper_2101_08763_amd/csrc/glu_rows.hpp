@@ -11,9 +11,10 @@
 // take blocks of 128 coordinates in turn, and their sums are added in order
 // through LDS at the end.  No temporary memory, and no order that a launch
 // changes.  One row by two bf16 weights of 8 192 x 4 096 that no cache holds takes 27.4
-// us (4.9 TB/s, a large copy's rate), one by 4 bits of 4 096 x 32 768 14 (5 TB/s); below
-// 30 MB the launch and the first loads are most of it (6.5 us for 4 096 x 8 192 by 4
-// bits, 3.1 at the copy's rate).  16 wavefronts to a workgroup spill.
+// us (4.9 TB/s, a large copy's rate), one by 4 bits of 4 096 x 131 072 57 (5 TB/s), of
+// 4 096 x 32 768 18 (4 TB/s); below 30 MB the launch and the first loads are most of it
+// (7.0 us for 4 096 x 8 192 by 4 bits, 3.1 at the copy's rate).  16 wavefronts to a workgroup
+// spill, and so does the block by 4 bits in groups of 32 with two tiles (w4_rows.hpp).
 //
 // Weights of 4 bits are whole numbers q = 0 .. 15 beside a scale s and a zero
 // point z per group: sum x w = s (sum x q - z sum x).  The byte 0x0q read as E4M3

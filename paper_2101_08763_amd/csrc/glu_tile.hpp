@@ -548,7 +548,8 @@ hipError_t dense_launch(DenseLaunch a, hipStream_t st) {
 
 // Tiles and splits for a product of M x N (pairs times), `stages` steps long, by an
 // estimate: 1.4 us a stage of the large tiles and 0.45 of the small ones, rounds of
-// workgroups over the CUs, and for splits of the sum their fp32 values written and
+// workgroups over the CUs (one to a CU, also of the small ones, of which two fit: a stage's
+// time is that of a CU with one), and for splits of the sum their fp32 values written and
 // read.  Measured, us, small and large tiles: block of bf16 100 x 1 536 x 4 096 14 / 33,
 // 2 000 x 1 536 x 4 096 70 / 45, 8 192 x 1 536 x 4 096 260 / 162, of fp32 128 x 1 024 x 2 048
 // 54 / 125; gradient of bf16 1 000 x 1 536 x 4 096 105 / 196, 8 192 x 1 536 x 4 096 906 / 412.

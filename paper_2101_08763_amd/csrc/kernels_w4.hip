@@ -19,7 +19,8 @@ constexpr float kLargest<__bf16> = 0x1.fep127f;
 // A wavefront takes a tile of 16 rows x 128 coordinates: lane (r, q) row r and the
 // coordinates 32 j + 8 q + e, which are its 16 bytes.  A group's extremes are those
 // of the lanes q of a row, over the j that belong to it.  HBM-bound: 32 768 rows of
-// 8 192 of bf16 by groups of 128 124 us (5.5 TB/s), of fp32 216 (5.6).
+// 8 192 of bf16 by groups of 128 124 us (5.5 TB/s), of fp32 217 (5.6), by groups of 32, with
+// four divisions for one, 137 and 228 (5.1, 5.4); 8 192 x 4 096 of bf16 20 and 23 (4.3, 3.8).
 template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void w4_quantize_kernel(const T *__restrict__ w, int64_t n, int64_t d, int64_t units,
                                                           u32x4 *__restrict__ codes, uint32_t *__restrict__ words) {
@@ -88,7 +89,8 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const T *__restrict__ 
 
 // A wavefront takes a tile, and each of its stores whole rows of it, 16 bytes a lane:
 // a lane's values are half a dword of codes (fp32) or a whole one.  HBM-bound: 32 768
-// rows of 4 096 to bf16 52 us (6.5 TB/s), to fp32 108 (5.6).  Lanes that take the 16
+// rows of 4 096 to bf16 52 us (6.5 TB/s), to fp32 108 (5.6); rows of 8 192 to bf16 124 (5.5),
+// to fp32, more than 0.8 GB of it, 290 (4.2).  Lanes that take the 16
 // bytes of codes in quantize's order store 64 bytes of a row at a time: 59 and, past
 // the caches, 247 us.
 template <typename T, bool STREAM>
@@ -146,8 +148,9 @@ hipError_t quantize(const void *w, int64_t n, int64_t d, int group, void *codes,
 }
 
 // Values that fill half the last-level cache (256 MiB) or more are stored past it (us,
-// through it and past it: 134 MB of fp32 38 / 26, 268 MB of bf16 67 / 52).  Fewer may be
-// read from it next.
+// through it and past it: 134 MB of fp32 38 / 26, of bf16 35 / 26, 537 MB 149 / 107 and
+// 126 / 124, 1.07 GB 300 / 290 and 248 / 242; 541 MB of bf16 rows of odd length 198 / 214).
+// Fewer may be read from it next.
 constexpr int64_t kStreamBytes = int64_t(128) << 20;
 
 template <typename T>

@@ -12,11 +12,11 @@
 //
 // What bounds it is the VALU beside the matrix cores: for 16 instructions on a group
 // of 128 a tile converts 32 pairs and applies scale and zero point with 16 FMAs.
-// 2 048 x 4 096 x 8 192 of bf16 by groups of 128 take 147 us, 0.93 PFLOP/s, the matrix
-// cores busy 46 % of the cycles; by 64 and 32 it takes 5 and 34 % more (twice and four
+// 2 048 x 4 096 x 8 192 of bf16 by groups of 128 take 142 us, 0.97 PFLOP/s, the matrix
+// cores busy 46 % of the cycles; by 64 and 32 it takes 5 and 32 % more (twice and four
 // times the scales and zero points), of fp32 2.2 times as long (three parts).  Leaving
 // out the FMAs, or the staging of x, would save a fifth each.  The VALU is busy 53 %,
-// and a wavefront waits for 30 % of its time: behind the barrier all read their next x
+// and a wavefront waits for 29 % of its time: behind the barrier all read their next x
 // together.  Registers for it twice, or a third wavefront to a SIMD, do not fit (256
 // are in use).  VALU and matrix phases held apart by barriers took 9 % more, and a
 // higher priority for half of the wavefronts or hints to the compiler's scheduling
